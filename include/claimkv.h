@@ -499,6 +499,146 @@ int claim_block_state_read(claim_pool* pool, uint32_t first, uint32_t count, uin
  * (Table 2: ambiguity yields no claim outcome rather than an error). */
 const char* claim_strerror(int status);
 
+/* ------------------------------------------------- sequences on a pool
+ *
+ * The calls below keep running sequences on the pool's blocks: they hand
+ * blocks out and take them back, write keys and values, and attend over
+ * them.  Everything about a sequence is device memory of the caller, changed
+ * by queued work only: no call waits for the stream or allocates, so all of
+ * them can be captured into a HIP graph.  Work is queued on the pool's
+ * stream.
+ *
+ * Sequence r has lengths[r] tokens; position p of it lies in block
+ * tables[r * max_blocks + p / block_size], at token p % block_size of the
+ * block; entries past its last block are CLAIM_NONE.  refs[b] counts the
+ * table entries that name block b: a block with refs 0 is free.  A program
+ * starts with tables all CLAIM_NONE, lengths and refs 0, and may hold blocks
+ * of its own (a claim's, until it is restored) by a count in refs.
+ *
+ * A block handed out (by grow, fork, compact) no longer holds the cache
+ * identity it was registered with: claim_lookup does not hit it.  A claim
+ * that recorded the block is judged as ever, by its own offload record. */
+typedef struct claim_seqs {
+  uint32_t max_seqs;   /* rows of tables */
+  uint32_t max_blocks; /* entries of a row */
+  uint32_t* tables;    /* [max_seqs][max_blocks] */
+  uint32_t* lengths;   /* [max_seqs] tokens */
+  uint32_t* refs;      /* [num_blocks] */
+  uint32_t* work;      /* scratch of CLAIM_SEQS_WORK(num_blocks, max_seqs) words */
+} claim_seqs;
+
+#define CLAIM_SEQS_WORK(num_blocks, max_seqs) (16 + 3 * (uint64_t)(num_blocks) + 4 * (uint64_t)(max_seqs))
+
+/* Status of one entry of a grow or fork (device memory). */
+#define CLAIM_SEQ_OK 0
+#define CLAIM_SEQ_NO_BLOCKS 1 /* not enough free blocks: the sequence is as before */
+#define CLAIM_SEQ_REFUSED 2   /* no such sequence, named twice, past max_blocks, or a child in use */
+
+/* ids: [n] rows of tables (NULL: rows 0..n-1), n <= max_seqs.
+ *
+ * claim_seqs_grow   lengths[ids[i]] += tokens[i], with the blocks that this
+ *                   takes: free blocks in ascending order, handed out in
+ *                   order of i, then of position.  Entry i gets its blocks
+ *                   if the blocks needed by entries 0..i do not exceed the
+ *                   free ones, else CLAIM_SEQ_NO_BLOCKS.  A row named twice
+ *                   grows by its first entry; the later one is refused.
+ * claim_seqs_fork   row children[i], which must be empty, becomes a copy of
+ *                   row parents[i]: full blocks are shared, and a partly
+ *                   filled last block is copied (in every plane) into a free
+ *                   block, lowest first, in order of i, so that the two
+ *                   sequences can go on writing.
+ * claim_seqs_free   gives up the rows' blocks: one count of each, the row
+ *                   CLAIM_NONE, its length 0.  Blocks keep their bytes.  A
+ *                   row named twice, or out of range, is passed over.
+ * claim_seqs_compact moves the blocks in use to the front of the pool: with
+ *                   U blocks in use, the i-th used block from U on (ascending)
+ *                   moves into the i-th free block below U; tables and refs
+ *                   follow.  *moved (device, may be NULL) = blocks moved.
+ *                   Claims name physical blocks: a claim whose blocks moved
+ *                   no longer finds its bytes there and fails closed.
+ * claim_blocks_copy copies block src[i] over block dst[i] in every plane.  No
+ *                   block may be written twice, or both written and read, in
+ *                   one call; pairs with a block >= num_blocks are passed over.
+ */
+int claim_seqs_grow(claim_pool* pool, const claim_seqs* seqs, const uint32_t* ids,
+                    const uint32_t* tokens, uint32_t n, uint32_t* status);
+int claim_seqs_fork(claim_pool* pool, const claim_seqs* seqs, const uint32_t* parents,
+                    const uint32_t* children, uint32_t n, uint32_t* status);
+int claim_seqs_free(claim_pool* pool, const claim_seqs* seqs, const uint32_t* ids, uint32_t n);
+int claim_seqs_compact(claim_pool* pool, const claim_seqs* seqs, uint32_t* moved);
+int claim_blocks_copy(claim_pool* pool, const uint32_t* src, const uint32_t* dst, uint32_t n);
+
+/* Rows of several heads in device memory, bf16: element (row, head, d) is
+ * data[row * row_stride + head * head_stride + d].  data is 16-byte aligned,
+ * strides (in elements) are multiples of 8, else EINVAL. */
+typedef struct claim_rows {
+  void* data;
+  uint64_t row_stride;
+  uint64_t head_stride;
+} claim_rows;
+
+/* Which rows belong to which sequences: sequence ids[s] (NULL: s) has rows
+ * offsets[s] .. offsets[s + 1) (NULL: row s alone, num_rows = num_seqs), its
+ * last ones: with n rows and length L, row i of it is position L - n + i.
+ * Layer l of a pool of K and V planes (planes_per_layer = 2) is meant.  A
+ * pool with elem_bytes 2 holds bf16, with elem_bytes 1 e4m3: a byte times
+ * k_scale or v_scale is the value (both must be finite and > 0; bf16 pools
+ * take 1). */
+typedef struct claim_kv_desc {
+  uint32_t layer;
+  uint32_t num_seqs;
+  uint32_t num_rows;
+  uint32_t reserved; /* must be 0 */
+  const uint32_t* ids;     /* [num_seqs] or NULL */
+  const uint32_t* offsets; /* [num_seqs + 1], ascending from 0 to num_rows, or NULL */
+  float k_scale;
+  float v_scale;
+} claim_kv_desc;
+
+/* Write rows of K and V (num_kv_heads heads of head_dim, a multiple of 8)
+ * into the blocks of their positions.  e4m3: x / scale, limited to +-448,
+ * rounded to nearest even (NaN stays NaN).  A row whose position has no block
+ * is not written. */
+int claim_kv_write(claim_pool* pool, const claim_seqs* seqs, const claim_kv_desc* kv,
+                   const claim_rows* k, const claim_rows* v);
+
+/* Attention of the rows' queries over their sequences' keys and values:
+ * query head h reads KV head h / (num_heads / num_kv_heads), and the row at
+ * position P sees positions 0..P:
+ *   out = sum_p w_p v_p / sum_p w_p,  w_p = exp(scale * q . k_p).
+ * A row that sees nothing (P < 0) gives 0.  A row that sees a position whose
+ * block is missing (CLAIM_NONE, >= num_blocks, or past the table) gives NaN:
+ * it fails closed.  Positions that a row does not see have no effect on it,
+ * whatever bytes they hold.  Scores, weights' sums and outputs are
+ * accumulated in 32 bits; the weights are rounded to bf16 for the product
+ * with V.
+ *
+ * With prefix_blocks > 0, positions 0 .. prefix_blocks * block_size - 1 of
+ * every sequence are read from `prefix` (what the tables hold there is not
+ * read), once for all sequences.
+ *
+ * head_dim is 64 or 128, num_heads a multiple of num_kv_heads, at most 64
+ * query heads to a KV head, else EINVAL.  work holds partial results:
+ * claim_attend_work bytes (it goes by max_blocks and the counts alone, not
+ * by lengths; it may be 0, work NULL), 256-byte aligned, used by this call
+ * only, in stream order. */
+typedef struct claim_attend_desc {
+  claim_kv_desc kv;
+  claim_rows q;
+  claim_rows out;
+  uint32_t num_heads;
+  uint32_t prefix_blocks;
+  const uint32_t* prefix; /* [prefix_blocks] */
+  float scale;            /* finite */
+  uint32_t reserved;      /* must be 0 */
+  void* work;
+  uint64_t work_bytes;
+} claim_attend_desc;
+
+int claim_attend_work(const claim_pool* pool, const claim_seqs* seqs, const claim_attend_desc* desc,
+                      uint64_t* bytes);
+int claim_attend(claim_pool* pool, const claim_seqs* seqs, const claim_attend_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

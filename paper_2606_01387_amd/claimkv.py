@@ -16,6 +16,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SOURCE = os.path.join(_HERE, "csrc", "claimkv.hip")
+SOURCES = (SOURCE, os.path.join(_HERE, "csrc", "blocks.hip"), os.path.join(_HERE, "csrc", "attend.hip"))
 LIBRARY = os.path.join(_HERE, "libclaimkv.so")
 INCLUDE = os.path.join(ROOT, "include")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -54,7 +55,9 @@ LOOKUP_DTYPE = np.dtype(
 EXPORTS = ("claim_pool_create", "claim_pool_destroy", "claim_offload", "claim_restore",
            "claim_staging_reset", "claim_check", "claim_check_static", "claim_lookup",
            "claim_identity_stats", "outcomes_read", "claim_timing_read", "claim_block_state_read",
-           "claim_digest_grid", "claim_strerror")
+           "claim_digest_grid", "claim_strerror", "claim_seqs_grow", "claim_seqs_fork",
+           "claim_seqs_free", "claim_seqs_compact", "claim_blocks_copy", "claim_kv_write",
+           "claim_attend", "claim_attend_work")
 
 
 class PoolDesc(ctypes.Structure):
@@ -96,6 +99,31 @@ class CGridInfo(ctypes.Structure):
                 ("pga", ctypes.c_uint32), ("groups", ctypes.c_uint32)]
 
 
+class CSeqs(ctypes.Structure):
+    _fields_ = [("max_seqs", ctypes.c_uint32), ("max_blocks", ctypes.c_uint32),
+                ("tables", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("work", ctypes.c_void_p)]
+
+
+class CRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_uint64),
+                ("head_stride", ctypes.c_uint64)]
+
+
+class CKvDesc(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_uint32), ("num_seqs", ctypes.c_uint32),
+                ("num_rows", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
+                ("ids", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
+class CAttendDesc(ctypes.Structure):
+    _fields_ = [("kv", CKvDesc), ("q", CRows), ("out", CRows), ("num_heads", ctypes.c_uint32),
+                ("prefix_blocks", ctypes.c_uint32), ("prefix", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_uint32),
+                ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_uint64)]
+
+
 assert ctypes.sizeof(PoolDesc) == 96 and ctypes.sizeof(CBatch) == 72
 assert OUTCOME_DTYPE.itemsize == 64 and EVENT_DTYPE.itemsize == 40 and LOOKUP_DTYPE.itemsize == 40
 
@@ -107,9 +135,14 @@ class ClaimError(RuntimeError):
 
 
 def build() -> str:
-    """Compile libclaimkv.so for gfx950 in-tree."""
+    """Compile libclaimkv.so for gfx950 in-tree, the sources side by side."""
     tmp = LIBRARY + ".tmp"
-    subprocess.run([HIPCC, *HIP_FLAGS, f"-I{INCLUDE}", SOURCE, "-o", tmp], check=True)
+    objects = [os.path.splitext(s)[0] + ".o" for s in SOURCES]
+    jobs = [subprocess.Popen([HIPCC, *(f for f in HIP_FLAGS if f != "-shared"), f"-I{INCLUDE}", "-c",
+                              s, "-o", o]) for s, o in zip(SOURCES, objects)]
+    if any([j.wait() for j in jobs]):  # every job ends before the first failure is told
+        raise RuntimeError(f"{HIPCC} failed")
+    subprocess.run([HIPCC, *HIP_FLAGS, *objects, "-o", tmp], check=True)
     os.replace(tmp, LIBRARY)
     return LIBRARY
 
@@ -141,6 +174,14 @@ def lib() -> ctypes.CDLL:
             "claim_block_state_read": ([vp, u32, u32, vp, vp, vp, vp], i32),
             "claim_digest_grid": ([vp, u64, ctypes.POINTER(CGridInfo)], i32),
             "claim_strerror": ([i32], ctypes.c_char_p),
+            "claim_seqs_grow": ([vp, vp, vp, vp, u32, vp], i32),
+            "claim_seqs_fork": ([vp, vp, vp, vp, u32, vp], i32),
+            "claim_seqs_free": ([vp, vp, vp, u32], i32),
+            "claim_seqs_compact": ([vp, vp, vp], i32),
+            "claim_blocks_copy": ([vp, vp, vp, u32], i32),
+            "claim_kv_write": ([vp, vp, vp, vp, vp], i32),
+            "claim_attend": ([vp, vp, vp], i32),
+            "claim_attend_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -424,10 +465,57 @@ class Pool:
         _check(lib().claim_digest_grid(self._h, n, ctypes.byref(g)), "claim_digest_grid")
         return {name: getattr(g, name) for name, _ in CGridInfo._fields_}
 
+    def copy_blocks(self, src, dst) -> None:
+        """claim_blocks_copy: block src[i] over block dst[i], in every plane
+        (int32 device tensors).  No block may be written twice, or both
+        written and read."""
+        _device_ints(self.kv.device, src=src, dst=dst)
+        if src.numel() != dst.numel():
+            raise ValueError("src and dst need one entry per copied block")
+        with self.ordered(src, dst):
+            _check(lib().claim_blocks_copy(self._h, src.data_ptr(), dst.data_ptr(), src.numel()),
+                   "claim_blocks_copy")
+
+    def ordered(self, *tensors):
+        """A with-block whose pool calls come after what the current stream
+        has queued, and before what it queues next, also where the pool's
+        stream is another one; ``tensors`` are the arguments of those calls."""
+        return _Ordered(self.stream, tensors)
+
     def timing(self) -> dict:
         t = CTiming()
         _check(lib().claim_timing_read(self._h, ctypes.byref(t)), "claim_timing_read")
         return {name: getattr(t, name) for name, _ in CTiming._fields_}
+
+
+class _Ordered:
+    __slots__ = ("stream", "current")
+
+    def __init__(self, stream, tensors):
+        self.stream = stream
+        self.current = _torch().cuda.current_stream(stream.device)
+        if self.current.cuda_stream == stream.cuda_stream:
+            self.current = None
+            return
+        stream.wait_stream(self.current)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        if self.current is not None:
+            self.current.wait_stream(self.stream)
+
+
+def _device_ints(device, **tensors) -> None:
+    """Each tensor (or None) is a contiguous int32 tensor on the device."""
+    torch = _torch()
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.int32 or t.device != device or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 tensor on {device}")
 
 
 def _staging_args(staging, nbytes):

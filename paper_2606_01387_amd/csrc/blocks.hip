@@ -1,0 +1,609 @@
+// blocks.hip -- sequences' blocks: growing, forking, freeing, compacting and
+// copying them, and writing keys and values into them (gfx950).
+//
+// The plans (which blocks go where) are whole numbers made by one workgroup:
+// every rank is a prefix sum, so results do not depend on the order in which
+// lanes or atomics run.  The bytes are moved by a second kernel over the
+// whole GPU that reads the plan from device memory; nothing comes back to the
+// host.
+
+#include "pool_view.h"
+
+namespace {
+
+constexpr uint32_t kNone = CLAIM_NONE;
+constexpr int kPlan = 1024;  // threads of a planning workgroup
+constexpr int kCopy = 256;   // threads of a copying workgroup
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+struct Seqs {
+  uint32_t max_seqs, max_blocks;
+  uint32_t *tables, *lengths, *refs;
+  // scratch: header (16 words), then three lists of num_blocks, then four of max_seqs
+  uint32_t *head, *list_a, *list_b, *map, *rank, *len, *owner, *need;
+};
+
+// header words
+enum : int { kPairs = 0, kUsed = 1 };
+
+Seqs seqs_dev(const claim_seqs* s, uint32_t nb) {
+  uint32_t* w = s->work;
+  uint32_t* q = w + 16 + 3 * (uint64_t)nb;
+  return Seqs{s->max_seqs, s->max_blocks, s->tables, s->lengths, s->refs, w,
+              w + 16, w + 16 + nb, w + 16 + 2 * (uint64_t)nb,
+              q, q + s->max_seqs, q + 2 * (uint64_t)s->max_seqs, q + 3 * (uint64_t)s->max_seqs};
+}
+
+// Exclusive prefix sum of one 64-bit value a thread over a planning
+// workgroup; *total is the sum.  Counts are summed in 64 bits: a request may
+// ask for far more blocks than there are.
+__device__ uint64_t block_scan(uint64_t v, uint64_t* total) {
+  __shared__ uint64_t wave_sum[kPlan / 64];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t y = __shfl_up(x, d);
+    if (lane >= (uint32_t)d) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) wave_sum[wave] = x;
+  __syncthreads();
+  uint64_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlan / 64; ++w) {
+    const uint64_t s = wave_sum[w];
+    all += s;
+    if (w < (int)wave) before += s;
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// This thread's contiguous share of the blocks: whole groups of 4.
+__device__ __forceinline__ void my_blocks(uint32_t nb, uint32_t* first, uint32_t* last) {
+  const uint32_t per = (nb / 4 / kPlan + 1) * 4;
+  const uint64_t f = (uint64_t)per * threadIdx.x;
+  *first = f < nb ? (uint32_t)f : nb;
+  *last = f + per < nb ? (uint32_t)(f + per) : nb;
+}
+
+__device__ uint32_t count_used(const uint32_t* refs, uint32_t first, uint32_t last) {
+  uint32_t used = 0, b = first;
+  if (((uintptr_t)refs & 15) == 0) {
+#pragma unroll 8
+    for (; b + 4 <= last; b += 4) {
+      const u32x4 r = *(const u32x4*)(refs + b);
+      used += (r.x != 0) + (r.y != 0) + (r.z != 0) + (r.w != 0);
+    }
+  }
+  for (; b < last; ++b) used += refs[b] != 0;
+  return used;
+}
+
+// The first `want` free blocks, ascending, into list; returns how many there
+// are free in all.
+__device__ uint64_t list_free(const uint32_t* refs, uint32_t nb, uint64_t want, uint32_t* list) {
+  uint32_t first, last;
+  my_blocks(nb, &first, &last);
+  uint64_t total;
+  uint64_t at = block_scan(last - first - count_used(refs, first, last), &total);
+  for (uint32_t b = first; b < last && at < want; ++b)
+    if (refs[b] == 0) list[at++] = b;
+  return total;
+}
+
+__device__ __forceinline__ uint32_t row_of(const uint32_t* ids, uint32_t i) { return ids ? ids[i] : i; }
+
+// owner[row] = the first i that names row (rows out of range have none).
+__device__ void first_owner(const Seqs& s, const uint32_t* ids, uint32_t n) {
+  for (uint32_t i = threadIdx.x; i < n; i += kPlan) {
+    const uint32_t r = row_of(ids, i);
+    if (r < s.max_seqs) s.owner[r] = kNone;
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n; i += kPlan) {
+    const uint32_t r = row_of(ids, i);
+    if (r < s.max_seqs) atomicMin(&s.owner[r], i);
+  }
+  __syncthreads();
+}
+
+// ---------------------------------------------------------------------- grow
+
+__global__ void __launch_bounds__(kPlan) k_grow(Seqs s, const uint32_t* ids, const uint32_t* tokens,
+                                                uint32_t n, uint32_t bs, uint32_t nb,
+                                                uint64_t* holder, uint32_t* status) {
+  first_owner(s, ids, n);
+  uint64_t run = 0;  // blocks that earlier entries need
+  for (uint32_t i0 = 0; i0 < n; i0 += kPlan) {
+    const uint32_t i = i0 + threadIdx.x;
+    uint64_t need = 0;
+    bool fine = false;
+    if (i < n) {
+      const uint32_t r = row_of(ids, i);
+      if (r < s.max_seqs && s.owner[r] == i) {
+        const uint64_t len = s.lengths[r], to = len + tokens[i];
+        fine = to <= (uint64_t)s.max_blocks * bs && to <= 0xFFFFFFFFull;
+        if (fine) need = (to + bs - 1) / bs - (len + bs - 1) / bs;
+      }
+    }
+    uint64_t total;
+    const uint64_t at = run + block_scan(need, &total);
+    if (i < n) {
+      // ranks past the blocks there are stay past them in 32 bits
+      s.rank[i] = at < nb ? (uint32_t)at : nb;
+      s.need[i] = fine ? (uint32_t)need : kNone;
+    }
+    run += total;
+  }
+  const uint64_t free_all = list_free(s.refs, nb, run, s.list_a);
+  __syncthreads();
+  // entries whose blocks are all there: a leading part of those that need any
+  uint64_t mine = 0;
+  for (uint32_t i = threadIdx.x; i < n; i += kPlan) {
+    const uint32_t need = s.need[i];
+    uint32_t st = CLAIM_SEQ_REFUSED;
+    if (need != kNone) {
+      const uint64_t end = (uint64_t)s.rank[i] + need;
+      st = end <= free_all ? CLAIM_SEQ_OK : CLAIM_SEQ_NO_BLOCKS;
+      if (st == CLAIM_SEQ_OK && need && end > mine) mine = end;
+      const uint32_t r = row_of(ids, i);
+      s.len[i] = s.lengths[r];
+      if (st == CLAIM_SEQ_OK) s.lengths[r] += tokens[i];
+    }
+    if (st != CLAIM_SEQ_OK) s.need[i] = 0;
+    if (status) status[i] = st;
+  }
+  __shared__ uint32_t given_all;
+  if (threadIdx.x == 0) given_all = 0;
+  __syncthreads();
+  if (mine) atomicMax(&given_all, (uint32_t)mine);
+  __syncthreads();
+  // block k goes to the last entry i with rank[i] <= k: ranks ascend, and an
+  // entry that needs none has the rank of the next
+  const uint32_t given = given_all;
+  for (uint32_t k = threadIdx.x; k < given; k += kPlan) {
+    uint32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (s.rank[mid] <= k) lo = mid; else hi = mid;
+    }
+    const uint32_t r = row_of(ids, lo), b = s.list_a[k];
+    const uint32_t at = (s.len[lo] + bs - 1) / bs + (k - s.rank[lo]);
+    s.tables[(uint64_t)r * s.max_blocks + at] = b;
+    s.refs[b] = 1;
+    holder[b] = 0;
+  }
+}
+
+// ---------------------------------------------------------------------- fork
+
+__global__ void __launch_bounds__(kPlan) k_fork_plan(Seqs s, const uint32_t* parents,
+                                                     const uint32_t* children, uint32_t n,
+                                                     uint32_t bs, uint32_t nb, uint64_t* holder,
+                                                     uint32_t* status) {
+  first_owner(s, children, n);
+  uint64_t run = 0;
+  for (uint32_t i0 = 0; i0 < n; i0 += kPlan) {
+    const uint32_t i = i0 + threadIdx.x;
+    uint64_t need = 0;
+    if (i < n) {
+      const uint32_t p = row_of(parents, i), c = row_of(children, i);
+      const bool fine = p < s.max_seqs && c < s.max_seqs && p != c && s.owner[c] == i &&
+                        s.lengths[c] == 0;
+      const uint32_t len = fine ? s.lengths[p] : 0;
+      need = len % bs != 0 && (uint64_t)len <= (uint64_t)s.max_blocks * bs;
+      s.len[i] = len;
+      s.need[i] = fine ? (uint32_t)need : kNone;
+    }
+    uint64_t total;
+    const uint64_t at = run + block_scan(need, &total);
+    if (i < n) s.rank[i] = (uint32_t)at;
+    run += total;
+  }
+  const uint64_t free_all = list_free(s.refs, nb, run, s.list_a);
+  if (threadIdx.x == 0) s.head[kPairs] = (uint32_t)(run < free_all ? run : free_all);
+  __syncthreads();  // parents' lengths are in s.len: children's may change now
+  for (uint32_t i = threadIdx.x; i < n; i += kPlan) {
+    const uint32_t need = s.need[i], len = s.len[i], rank = s.rank[i];
+    uint32_t st = CLAIM_SEQ_REFUSED;
+    if (need != kNone) st = (uint64_t)rank + need <= free_all ? CLAIM_SEQ_OK : CLAIM_SEQ_NO_BLOCKS;
+    if (status) status[i] = st;
+    if (st != CLAIM_SEQ_OK) {
+      s.len[i] = 0;  // shares nothing
+      continue;
+    }
+    const uint32_t p = row_of(parents, i), c = row_of(children, i);
+    s.lengths[c] = len;
+    if (need) {
+      const uint32_t at = len / bs;
+      const uint32_t from = s.tables[(uint64_t)p * s.max_blocks + at], to = s.list_a[rank];
+      s.list_b[rank] = from;  // a missing one is passed over by the copy
+      if (from < nb) {
+        s.tables[(uint64_t)c * s.max_blocks + at] = to;
+        s.refs[to] = 1;
+        holder[to] = 0;
+      }
+    }
+  }
+}
+
+// One contiguous piece of a block's chunk in one plane, `n` 16-byte words:
+// eight loads of a thread are in flight before its first store.
+__device__ __forceinline__ void copy_words(const u32x4* __restrict__ src, u32x4* __restrict__ dst,
+                                           uint32_t n) {
+  uint32_t v = threadIdx.x;
+  for (; v + 7 * kCopy < n; v += 8 * kCopy) {
+    u32x4 r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = src[v + j * kCopy];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dst[v + j * kCopy] = r[j];
+  }
+  u32x4 r[7];
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (v + j * kCopy < n) r[j] = src[v + j * kCopy];
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (v + j * kCopy < n) dst[v + j * kCopy] = r[j];
+}
+
+struct CopyShape {
+  uint32_t planes, nb, pieces, piece_words, words;  // words of a chunk
+};
+
+__device__ void copy_pairs(u32x4* kv, const CopyShape& c, const uint32_t* src, const uint32_t* dst,
+                           uint32_t pairs, uint32_t first, uint32_t stride) {
+  const uint64_t items = (uint64_t)pairs * c.planes * c.pieces;
+  for (uint64_t it = first; it < items; it += stride) {
+    const uint32_t piece = (uint32_t)(it % c.pieces);
+    const uint64_t rest = it / c.pieces;
+    const uint32_t pair = (uint32_t)(rest % pairs), plane = (uint32_t)(rest / pairs);
+    const uint32_t a = src[pair], b = dst[pair];
+    if (a >= c.nb || b >= c.nb) continue;
+    const uint32_t w0 = piece * c.piece_words;
+    const uint32_t n = c.words - w0 < c.piece_words ? c.words - w0 : c.piece_words;
+    const uint64_t row = (uint64_t)plane * c.nb;
+    copy_words(kv + (row + a) * c.words + w0, kv + (row + b) * c.words + w0, n);
+  }
+}
+
+// The first n workgroups share the full blocks of one child each; all of them
+// copy.
+__global__ void __launch_bounds__(kCopy) k_fork_apply(Seqs s, const uint32_t* parents,
+                                                      const uint32_t* children, uint32_t n,
+                                                      uint32_t bs, CopyShape c, u32x4* kv) {
+  for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
+    uint32_t full = s.len[i] / bs;
+    if (full == 0) continue;
+    if (full > s.max_blocks) full = s.max_blocks;
+    const uint32_t* from = s.tables + (uint64_t)row_of(parents, i) * s.max_blocks;
+    uint32_t* to = s.tables + (uint64_t)row_of(children, i) * s.max_blocks;
+    for (uint32_t j = threadIdx.x; j < full; j += kCopy) {
+      const uint32_t b = from[j];
+      to[j] = b;
+      if (b < c.nb) atomicAdd(&s.refs[b], 1u);
+    }
+  }
+  copy_pairs(kv, c, s.list_b, s.list_a, s.head[kPairs], blockIdx.x, gridDim.x);
+}
+
+__global__ void __launch_bounds__(kCopy) k_copy(const uint32_t* src, const uint32_t* dst,
+                                                uint32_t n, CopyShape c, u32x4* kv,
+                                                uint64_t* holder) {
+  if (blockIdx.x == 0)
+    for (uint32_t i = threadIdx.x; i < n; i += kCopy)
+      if (src[i] < c.nb && dst[i] < c.nb) holder[dst[i]] = 0;
+  copy_pairs(kv, c, src, dst, n, blockIdx.x, gridDim.x);
+}
+
+// ---------------------------------------------------------------------- free
+
+__global__ void __launch_bounds__(kCopy) k_free(Seqs s, const uint32_t* ids, uint32_t bs,
+                                                uint32_t nb) {
+  const uint32_t r = row_of(ids, blockIdx.x);
+  if (r >= s.max_seqs) return;
+  __shared__ uint32_t len;
+  if (threadIdx.x == 0) len = atomicExch(&s.lengths[r], 0u);  // a row named twice is freed once
+  __syncthreads();
+  if (len == 0) return;
+  const uint64_t blocks = ((uint64_t)len + bs - 1) / bs;
+  uint32_t* row = s.tables + (uint64_t)r * s.max_blocks;
+  for (uint32_t j = threadIdx.x; j < s.max_blocks; j += kCopy) {
+    if (j < blocks) {
+      const uint32_t b = row[j];
+      if (b < nb) {  // a count that is 0 already stays 0
+        uint32_t old = s.refs[b];
+        while (old) {
+          const uint32_t seen = atomicCAS(&s.refs[b], old, old - 1);
+          if (seen == old) break;
+          old = seen;
+        }
+      }
+    }
+    row[j] = kNone;
+  }
+}
+
+// ------------------------------------------------------------------- compact
+
+__global__ void __launch_bounds__(kPlan) k_compact_plan(Seqs s, uint32_t nb, uint64_t* holder,
+                                                        uint32_t* moved) {
+  __shared__ uint32_t used_below;  // blocks in use below U
+  uint32_t first, last;
+  my_blocks(nb, &first, &last);
+  uint64_t total;
+  const uint32_t before = (uint32_t)block_scan(count_used(s.refs, first, last), &total);
+  const uint32_t U = (uint32_t)total;
+  if (threadIdx.x == 0) used_below = U;  // U = nb: nobody's share holds block U
+  __syncthreads();
+  if (first <= U && U < last) used_below = before + count_used(s.refs, first, U);
+  __syncthreads();
+  const uint32_t low = used_below, pairs = U - low;
+  uint32_t used = before;
+  for (uint32_t b = first; b < last; ++b) {
+    const bool in_use = s.refs[b] != 0;
+    if (b < U) {
+      if (!in_use) s.list_a[b - used] = b;
+    } else {
+      s.map[b] = kNone;  // an entry that names a block with no count names nothing
+      if (in_use) s.list_b[used - low] = b;
+    }
+    used += in_use;
+  }
+  if (threadIdx.x == 0) {
+    s.head[kPairs] = pairs;
+    s.head[kUsed] = U;
+    if (moved) *moved = pairs;
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < pairs; i += kPlan) {
+    const uint32_t to = s.list_a[i], from = s.list_b[i];
+    s.map[from] = to;
+    s.refs[to] = s.refs[from];
+    s.refs[from] = 0;
+    holder[to] = 0;
+  }
+}
+
+__global__ void __launch_bounds__(kCopy) k_compact_apply(Seqs s, CopyShape c, u32x4* kv) {
+  const uint32_t pairs = s.head[kPairs], U = s.head[kUsed];
+  if (pairs == 0) return;
+  const uint64_t entries = (uint64_t)s.max_seqs * s.max_blocks;
+  for (uint64_t i = (uint64_t)blockIdx.x * kCopy + threadIdx.x; i < entries;
+       i += (uint64_t)gridDim.x * kCopy) {
+    const uint32_t b = s.tables[i];
+    if (b >= U && b < c.nb) s.tables[i] = s.map[b];
+  }
+  copy_pairs(kv, c, s.list_b, s.list_a, pairs, blockIdx.x, gridDim.x);
+}
+
+// --------------------------------------------------------------------- write
+
+struct WriteArgs {
+  uint32_t num_seqs, rows, vecs, head_vecs;  // 8-element vectors of a row, of a head
+  const uint32_t *ids, *offsets;
+  const uint16_t *k, *v;
+  uint64_t k_row, k_head, v_row, v_head;  // strides in elements
+  float k_scale, v_scale;
+  uint32_t bs, nb;
+  uint64_t chunk_bytes;
+  uint8_t *k_plane, *v_plane;
+};
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// x / scale limited to the largest e4m3 value; NaN passes through.
+__device__ __forceinline__ float limit_e4m3(float x, float scale) {
+  x = x / scale;
+  x = x > 448.0f ? 448.0f : x;
+  return x < -448.0f ? -448.0f : x;
+}
+
+// Four bf16 values (two words) to four e4m3 bytes, to nearest even.
+__device__ __forceinline__ uint32_t to_e4m3(uint32_t w0, uint32_t w1, float scale) {
+  int p = __builtin_amdgcn_cvt_pk_fp8_f32(limit_e4m3(bf16_lo(w0), scale),
+                                          limit_e4m3(bf16_hi(w0), scale), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(limit_e4m3(bf16_lo(w1), scale),
+                                                   limit_e4m3(bf16_hi(w1), scale), p, true);
+}
+
+// A wave takes one row; its lanes take the row's 16-byte vectors, first K's,
+// then V's.
+template <bool E4M3>
+__global__ void __launch_bounds__(256) k_write(WriteArgs a, Seqs s) {
+  const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= a.rows) return;
+  uint32_t q = row, i = 0, n = 1;
+  if (a.offsets) {
+    q = wave_find_seq(a.offsets, a.num_seqs, row);
+    const uint32_t o = a.offsets[q], e = a.offsets[q + 1];
+    if (o > row || e <= row) return;  // offsets that do not hold the row
+    i = row - o;
+    n = e - o;
+  }
+  const uint32_t r = a.ids ? a.ids[q] : q;
+  if (r >= s.max_seqs) return;
+  const int64_t pos = (int64_t)s.lengths[r] - n + i;
+  if (pos < 0) return;
+  const uint32_t at = (uint32_t)pos / a.bs, token = (uint32_t)pos % a.bs;
+  if (at >= s.max_blocks) return;
+  const uint32_t b = s.tables[(uint64_t)r * s.max_blocks + at];
+  if (b >= a.nb) return;
+  const uint64_t base = (uint64_t)b * a.chunk_bytes;
+  for (uint32_t x = lane; x < 2 * a.vecs; x += 64) {
+    const bool is_v = x >= a.vecs;
+    const uint32_t v = is_v ? x - a.vecs : x;
+    const uint32_t head = v / a.head_vecs, d = v % a.head_vecs;
+    const uint16_t* src = is_v ? a.v + row * a.v_row + head * a.v_head
+                               : a.k + row * a.k_row + head * a.k_head;
+    const u32x4 w = *(const u32x4*)(src + 8 * d);
+    uint8_t* dst = (is_v ? a.v_plane : a.k_plane) + base;
+    const uint64_t vec = (uint64_t)token * a.vecs + v;
+    if (E4M3) {
+      const float scale = is_v ? a.v_scale : a.k_scale;
+      *(u32x2*)(dst + vec * 8) = u32x2{to_e4m3(w.x, w.y, scale), to_e4m3(w.z, w.w, scale)};
+    } else {
+      *(u32x4*)(dst + vec * 16) = w;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------- host
+
+CopyShape copy_shape(const PoolView& p) {
+  CopyShape c;
+  c.planes = p.layers * p.planes_per_layer;
+  c.nb = p.nb;
+  c.words = (uint32_t)(p.chunk_bytes / 16);
+  const uint32_t most = 8 * kCopy;  // 32 KiB: one round of eight loads a thread
+  c.pieces = (c.words + most - 1) / most;
+  c.piece_words = (c.words + c.pieces - 1) / c.pieces;
+  return c;
+}
+
+// Workgroups for at most `items` pieces: eight to a CU read the plan's
+// counts and share what there is.
+uint32_t copy_grid(const PoolView& p, uint64_t items) {
+  const uint64_t most = 8ull * p.cus;
+  return (uint32_t)(items < 1 ? 1 : items < most ? items : most);
+}
+
+int launched() {
+  if (hipGetLastError() != hipSuccess) return CLAIM_EHIP;
+  return CLAIM_OK;
+}
+
+int check_planned(const claim_pool* P, const claim_seqs* s, uint32_t n) {
+  if (!P) return CLAIM_EINVAL;
+  const int rc = check_seqs(s);
+  if (rc != CLAIM_OK) return rc;
+  return !s->work || n > s->max_seqs ? CLAIM_EINVAL : CLAIM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int claim_seqs_grow(claim_pool* P, const claim_seqs* s, const uint32_t* ids, const uint32_t* tokens,
+                    uint32_t n, uint32_t* status) {
+  const int rc = check_planned(P, s, n);
+  if (rc != CLAIM_OK || (n && !tokens)) return rc != CLAIM_OK ? rc : CLAIM_EINVAL;
+  if (n == 0) return CLAIM_OK;
+  const PoolView p = pool_view(P);
+  SEQ_HIP(hipSetDevice(p.device));
+  hipLaunchKernelGGL(k_grow, dim3(1), dim3(kPlan), 0, p.stream, seqs_dev(s, p.nb), ids, tokens, n,
+                     p.bs, p.nb, p.holder, status);
+  return launched();
+}
+
+int claim_seqs_fork(claim_pool* P, const claim_seqs* s, const uint32_t* parents,
+                    const uint32_t* children, uint32_t n, uint32_t* status) {
+  const int rc = check_planned(P, s, n);
+  if (rc != CLAIM_OK || (n && (!parents || !children))) return rc != CLAIM_OK ? rc : CLAIM_EINVAL;
+  if (n == 0) return CLAIM_OK;
+  const PoolView p = pool_view(P);
+  SEQ_HIP(hipSetDevice(p.device));
+  const Seqs d = seqs_dev(s, p.nb);
+  hipLaunchKernelGGL(k_fork_plan, dim3(1), dim3(kPlan), 0, p.stream, d, parents, children, n, p.bs,
+                     p.nb, p.holder, status);
+  const CopyShape c = copy_shape(p);
+  hipLaunchKernelGGL(k_fork_apply, dim3(copy_grid(p, (uint64_t)n * c.planes * c.pieces)),
+                     dim3(kCopy), 0, p.stream, d, parents, children, n, p.bs, c, (u32x4*)p.kv);
+  return launched();
+}
+
+int claim_seqs_free(claim_pool* P, const claim_seqs* s, const uint32_t* ids, uint32_t n) {
+  if (!P) return CLAIM_EINVAL;
+  const int rc = check_seqs(s);
+  if (rc != CLAIM_OK || n > s->max_seqs) return rc != CLAIM_OK ? rc : CLAIM_EINVAL;
+  if (n == 0) return CLAIM_OK;
+  const PoolView p = pool_view(P);
+  SEQ_HIP(hipSetDevice(p.device));
+  Seqs d{};
+  d.max_seqs = s->max_seqs;
+  d.max_blocks = s->max_blocks;
+  d.tables = s->tables;
+  d.lengths = s->lengths;
+  d.refs = s->refs;
+  hipLaunchKernelGGL(k_free, dim3(n), dim3(kCopy), 0, p.stream, d, ids, p.bs, p.nb);
+  return launched();
+}
+
+int claim_seqs_compact(claim_pool* P, const claim_seqs* s, uint32_t* moved) {
+  const int rc = check_planned(P, s, 0);
+  if (rc != CLAIM_OK) return rc;
+  const PoolView p = pool_view(P);
+  SEQ_HIP(hipSetDevice(p.device));
+  const Seqs d = seqs_dev(s, p.nb);
+  hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kPlan), 0, p.stream, d, p.nb, p.holder, moved);
+  const CopyShape c = copy_shape(p);
+  const uint64_t most = (uint64_t)(p.nb / 2 + 1) * c.planes * c.pieces;
+  hipLaunchKernelGGL(k_compact_apply, dim3(copy_grid(p, most)), dim3(kCopy), 0, p.stream, d, c,
+                     (u32x4*)p.kv);
+  return launched();
+}
+
+int claim_blocks_copy(claim_pool* P, const uint32_t* src, const uint32_t* dst, uint32_t n) {
+  if (!P || (n && (!src || !dst))) return CLAIM_EINVAL;
+  const PoolView p = pool_view(P);
+  if (n > p.nb) return CLAIM_EINVAL;  // some block would be written twice
+  if (n == 0) return CLAIM_OK;
+  SEQ_HIP(hipSetDevice(p.device));
+  const CopyShape c = copy_shape(p);
+  hipLaunchKernelGGL(k_copy, dim3(copy_grid(p, (uint64_t)n * c.planes * c.pieces)), dim3(kCopy), 0,
+                     p.stream, src, dst, n, c, (u32x4*)p.kv, p.holder);
+  return launched();
+}
+
+int claim_kv_write(claim_pool* P, const claim_seqs* s, const claim_kv_desc* kv, const claim_rows* k,
+                   const claim_rows* v) {
+  if (!P || !kv || !k || !v) return CLAIM_EINVAL;
+  const PoolView p = pool_view(P);
+  int rc = check_seqs(s);
+  if (rc == CLAIM_OK) rc = check_kv(p, s, kv);
+  if (rc != CLAIM_OK) return rc;
+  if (p.dim % 8) return CLAIM_EINVAL;
+  if (kv->num_rows == 0) return CLAIM_OK;
+  if (!rows_ok(*k) || !rows_ok(*v)) return CLAIM_EINVAL;
+  SEQ_HIP(hipSetDevice(p.device));
+  WriteArgs a;
+  a.num_seqs = kv->num_seqs;
+  a.rows = kv->num_rows;
+  a.head_vecs = p.dim / 8;
+  a.vecs = p.heads * a.head_vecs;
+  a.ids = kv->ids;
+  a.offsets = kv->offsets;
+  a.k = (const uint16_t*)k->data;
+  a.v = (const uint16_t*)v->data;
+  a.k_row = k->row_stride;
+  a.k_head = k->head_stride;
+  a.v_row = v->row_stride;
+  a.v_head = v->head_stride;
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.bs = p.bs;
+  a.nb = p.nb;
+  a.chunk_bytes = p.chunk_bytes;
+  const uint64_t plane = (uint64_t)p.nb * p.chunk_bytes;
+  a.k_plane = p.kv + 2ull * kv->layer * plane;
+  a.v_plane = a.k_plane + plane;
+  Seqs d{};
+  d.max_seqs = s->max_seqs;
+  d.max_blocks = s->max_blocks;
+  d.tables = s->tables;
+  d.lengths = s->lengths;
+  const dim3 grid((kv->num_rows + 3) / 4);
+  if (p.elem == 1)
+    hipLaunchKernelGGL(k_write<true>, grid, dim3(256), 0, p.stream, a, d);
+  else
+    hipLaunchKernelGGL(k_write<false>, grid, dim3(256), 0, p.stream, a, d);
+  return launched();
+}
+
+}  // extern "C"

@@ -59,6 +59,7 @@
 #include <new>
 
 #include "claimkv.h"
+#include "pool_view.h"
 
 namespace {
 
@@ -2558,6 +2559,7 @@ struct claim_pool {
   uint32_t cus = 256;
 
   uint32_t planes = 0, bs = 0, nb = 0;
+  uint32_t layers = 0, planes_per_layer = 0, heads = 0, dim = 0, elem = 0;
   uint64_t chunk_bytes = 0, chunk_vecs = 0, block_bytes = 0, seed = 0;
   KeyMap kmap{};  // key positions (head shards)
   void* kv = nullptr;
@@ -3389,6 +3391,11 @@ int record_stage(claim_pool* P, int slot, int stage) {
 
 }  // namespace
 
+PoolView pool_view(const claim_pool* P) {
+  return PoolView{P->device, P->stream, P->cus,  P->layers,      P->planes_per_layer, P->bs,    P->heads,
+                  P->dim,    P->elem,   P->nb,   P->chunk_bytes, (uint8_t*)P->kv,     P->holder};
+}
+
 extern "C" {
 
 const char* claim_strerror(int status) {
@@ -3449,6 +3456,11 @@ int claim_pool_create(const claim_pool_desc* d, claim_pool** out) {
     P->planes = (uint32_t)planes;
     P->bs = d->block_size;
     P->nb = d->num_blocks;
+    P->layers = d->num_layers;
+    P->planes_per_layer = d->planes_per_layer;
+    P->heads = d->num_kv_heads;
+    P->dim = d->head_dim;
+    P->elem = d->elem_bytes;
     P->chunk_bytes = chunk;
     P->chunk_vecs = chunk / 16;
     P->block_bytes = planes * chunk;

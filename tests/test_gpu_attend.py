@@ -1,0 +1,249 @@
+"""Attention over a pool's blocks against the definition in 64 bits."""
+
+import numpy as np
+import pytest
+
+from attend_world import World, check
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(ck, w, prefix=False, stream=None, **kw):
+    pool, seqs, d = w.to_gpu(ck, stream)
+    with pool:
+        if prefix:
+            return seqs.attend_shared(w.layer, d.q, d.prefix, offsets=d.offsets, **w.scales(), **kw).cpu()
+        return seqs.attend(w.layer, d.q, offsets=d.offsets, **w.scales(), **kw).cpu()
+
+
+# (rows, tokens cached before them): prompts from one token on, rows with
+# nothing before them, sequences with no rows, ends inside blocks and tiles
+PROMPTS = {
+    "one": [(1, 0)],
+    "short": [(3, 0), (1, 7), (0, 5), (16, 0), (17, 1)],
+    "tile-edges": [(32, 0), (33, 31), (64, 0), (63, 1), (65, 64)],
+    "long": [(257, 0), (5, 300), (130, 77)],
+    "few-after-many": [(2, 700), (1, 65)],
+}
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("seqs", PROMPTS.values(), ids=PROMPTS)
+def test_prompts(torch, ck, seqs, dim, e4m3):
+    w = World(torch, seqs=seqs, dim=dim, e4m3=e4m3, seed=1)
+    check(attend(ck, w), *w.expected())
+
+
+@pytest.mark.parametrize("block_size", [1, 5, 8, 24, 64, 100])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_block_sizes(torch, ck, block_size, dim):
+    if block_size * dim * 2 * 3 % 16:
+        pytest.skip("chunks are multiples of 16 bytes")
+    w = World(torch, seqs=[(40, 0), (1, 70), (9, 130)], heads=3, block_size=block_size, dim=dim, seed=2)
+    check(attend(ck, w), *w.expected())
+
+
+@pytest.mark.parametrize("heads,group", [(1, 1), (1, 16), (2, 5), (3, 7), (8, 4), (1, 33), (1, 64)])
+def test_head_groups(torch, ck, heads, group):
+    w = World(torch, seqs=[(9, 20), (1, 50), (40, 3)], heads=heads, group=group, seed=3)
+    check(attend(ck, w), *w.expected())
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("seqs,blocks", [
+    ([(1, 0)], 1), ([(1, 3), (1, 40), (1, 0)], 3), ([(1, 9)] * 40, 20), ([(2, 9), (1, 0), (3, 100)], 40),
+    ([(1, 200)] * 3, 0), ([(60, 0), (1, 5)], 7)], ids=str)
+def test_shared_prefix(torch, ck, seqs, blocks, dim, e4m3):
+    w = World(torch, seqs=seqs, dim=dim, e4m3=e4m3, prefix_blocks=blocks, group=4, seed=4)
+    check(attend(ck, w, prefix=True), *w.expected())
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("seqs", [[(1, 5000)], [(1, 3000), (1, 1), (1, 800)], [(20, 4000)]], ids=str)
+def test_long_axis_is_split(torch, ck, seqs, e4m3):
+    w = World(torch, seqs=seqs, heads=1, group=8, dim=128, e4m3=e4m3, seed=5)
+    check(attend(ck, w), *w.expected())
+
+
+def test_rows_shorter_than_their_prefix(torch, ck):
+    """A length inside the prefix (or 0) sees that much of it."""
+    w = World(torch, seqs=[(1, 5), (1, 0), (1, 0), (1, 0)], prefix_blocks=6, group=4, seed=6)
+    w.length[1], w.length[2], w.length[3] = 0, 1, 50
+    w.lengths = torch.tensor(w.length, dtype=torch.int32)
+    expected = w.expected()
+    assert (expected[0][1] == 0).all()
+    check(attend(ck, w, prefix=True), *expected)
+
+
+def test_more_rows_than_tokens(torch, ck):
+    """Rows before position 0 see nothing and give 0."""
+    w = World(torch, seqs=[(40, 0), (3, 10)], seed=7)
+    w.length[0] = 11
+    w.lengths = torch.tensor(w.length, dtype=torch.int32)
+    expected = w.expected()
+    assert (expected[0][:29] == 0).all() and (expected[0][29] != 0).any()
+    check(attend(ck, w), *expected)
+
+
+@pytest.mark.parametrize("kind", ["none", "out of range", "past the table"])
+@pytest.mark.parametrize("seqs", [[(70, 30), (5, 0)], [(1, 99), (1, 4)]], ids=str)
+def test_a_missing_block_is_nan(torch, ck, seqs, kind):
+    """Rows that see a position without a block are NaN, the others exact."""
+    w = World(torch, seqs=seqs, seed=8)
+    if kind == "past the table":
+        w.tables = w.tables[:, :4].contiguous()
+    else:
+        w.tables[0, 4] = -1 if kind == "none" else w.blocks
+    expected = w.expected()
+    assert np.isnan(expected[0]).any() and not np.isnan(expected[0][-1]).any()
+    check(attend(ck, w), *expected)
+
+
+def test_a_missing_prefix_block_is_nan(torch, ck):
+    w = World(torch, seqs=[(1, 3), (1, 0)], prefix_blocks=4, seed=9)
+    w.prefix[2] = -1
+    w.length[1] = 20
+    w.lengths = torch.tensor(w.length, dtype=torch.int32)
+    expected = w.expected()
+    assert np.isnan(expected[0][0]).all() and not np.isnan(expected[0][1]).any()
+    check(attend(ck, w, prefix=True), *expected)
+
+
+def test_a_wild_length_ends(torch, ck):
+    """A length far past the table is NaN, at once."""
+    w = World(torch, seqs=[(1, 40), (1, 7)], seed=10)
+    expected, bound = w.expected()
+    w.lengths = torch.tensor([2**31 - 1, 8], dtype=torch.int32)
+    expected[0] = np.nan
+    check(attend(ck, w), expected, bound)
+
+
+@pytest.mark.parametrize("plane", [0, 1])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("seqs", [[(90, 10)], [(4, 60)]], ids=str)
+def test_hidden_values_have_no_effect(torch, ck, seqs, value, plane):
+    """An infinity or NaN in a key or value that only later rows see."""
+    w = World(torch, seqs=seqs, seed=11)
+    clean, bound = w.expected()
+    pos = w.length[0] - 2  # the last two rows see it
+    w.kv[2 * w.layer + plane, w.tables[0, pos // w.bs], pos % w.bs, 0, 5] = value
+    got = attend(ck, w).double().numpy()
+    rows = w.rows - 2
+    off = np.abs(got[:rows] - clean[:rows])
+    assert (off <= bound[:rows]).all()
+    if plane == 1:  # a value: its one column in the rows and heads that see it
+        assert not np.isfinite(got[rows:, :w.group, 5]).any()
+        rest = np.abs(got[rows:] - clean[rows:])
+        rest[:, :w.group, 5] = 0
+        assert (rest <= bound[rows:]).all()
+    elif value != value:
+        assert np.isnan(got[rows:, :w.group]).all()
+
+
+def test_extreme_scores(torch, ck):
+    """Scores of many thousands: one key takes all; and equal scores: the mean."""
+    w = World(torch, seqs=[(70, 100), (1, 300)], spread=30.0, seed=12)
+    check(attend(ck, w), *w.expected())
+    w = World(torch, seqs=[(70, 100)], seed=13)
+    w.q.zero_()
+    check(attend(ck, w), *w.expected())
+
+
+def test_a_scale_of_ones_own(torch, ck):
+    w = World(torch, seqs=[(20, 50)], seed=14)
+    check(attend(ck, w, scale=0.5), *w.expected(0.5))
+    check(attend(ck, w, scale=1e-30), *w.expected(1e-30))
+
+
+def test_strided_rows_ids_and_out(torch, ck):
+    """Queries sliced from a wider projection, heads outermost, sequences
+    chosen by ids, the output a slice too."""
+    w = World(torch, seqs=[(5, 30), (9, 0), (1, 77)], heads=2, group=3, dim=64, seed=15)
+    pool, seqs, d = w.to_gpu(ck)
+    expected, bound = w.expected()
+    with pool:
+        wide = torch.zeros(w.rows, 2, 10, 64, dtype=torch.bfloat16, device="cuda")
+        wide[:, 1, 2:8] = d.q
+        out = torch.full((6, w.rows, 64), 7.0, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+        got = seqs.attend(w.layer, wide[:, 1, 2:8], offsets=d.offsets, out=out)
+        assert got is out
+        check(got, expected, bound)
+        # the same sequences in another order of table rows
+        order = torch.tensor([2, 0, 1], device="cuda")
+        seqs.tables.copy_(seqs.tables[order])
+        seqs.lengths.copy_(seqs.lengths[order])
+        ids = torch.tensor([1, 2, 0], dtype=torch.int32, device="cuda")
+        check(seqs.attend(w.layer, d.q, ids=ids, offsets=d.offsets), expected, bound)
+
+
+def test_another_stream(torch, ck):
+    """Tensors made on the current stream, a pool on another."""
+    w = World(torch, seqs=[(300, 500), (1, 900)], heads=2, group=4, dim=128, seed=16)
+    expected, bound = w.expected()
+    pool, seqs, d = w.to_gpu(ck, torch.cuda.Stream())
+    with pool:
+        for _ in range(4):
+            q = d.q * 1  # queued on the current stream just before
+            out = seqs.attend(w.layer, q, offsets=d.offsets) + 0
+            del q
+            check(out, expected, bound)
+
+
+def test_graph_replays(torch, ck):
+    """A decoding step captured once and replayed as the sequences grow."""
+    w = World(torch, seqs=[(1, 700), (1, 40)], heads=2, group=4, dim=128, prefix_blocks=20, seed=17)
+    stream = torch.cuda.Stream()
+    pool, seqs, d = w.to_gpu(ck, stream)
+    with pool, torch.cuda.stream(stream):
+        eager = seqs.attend_shared(w.layer, d.q, d.prefix)  # sizes the scratch
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = seqs.attend_shared(w.layer, d.q, d.prefix)
+        for length in (w.length, [w.length[0] - 3, w.length[1] - 7], w.length):
+            seqs.lengths.copy_(torch.tensor(length, dtype=torch.int32))
+            graph.replay()
+            got = out.clone()
+            eager = seqs.attend_shared(w.layer, d.q, d.prefix)
+            torch.cuda.synchronize()
+            assert torch.equal(got, eager)
+        check(eager, *w.expected())
+
+
+def test_same_bits_every_time(torch, ck):
+    w = World(torch, seqs=[(1, 3000), (40, 200)], heads=1, group=8, dim=128, prefix_blocks=30, seed=18)
+    pool, seqs, d = w.to_gpu(ck)
+    with pool:
+        first = seqs.attend_shared(w.layer, d.q, d.prefix, offsets=d.offsets)
+        for _ in range(5):
+            assert torch.equal(first, seqs.attend_shared(w.layer, d.q, d.prefix, offsets=d.offsets))
+
+
+def test_blocks_past_32_bits(torch, ck):
+    """A plane of over 4 GiB, a table row in its last blocks, the last layer."""
+    from paper_2606_01387_amd.sequences import Sequences
+    from paper_2606_01387_amd.synth import Geometry
+
+    heads, dim, bs, blocks, L = 8, 128, 16, 140000, 77
+    kv = torch.zeros(2, blocks, bs, heads, dim, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(19)
+    table = torch.arange(blocks - 5, blocks, dtype=torch.int32).flip(0)[None]
+    data = torch.randn(2, L, heads, dim, generator=g).to(torch.bfloat16)
+    k, v = data[0].cuda(), data[1].cuda()
+    with ck.Pool(Geometry(1, 2, bs, heads, dim, 2, blocks), 3, kv.view(torch.uint8), max_claims=16,
+                 max_footprint=64, event_capacity=64) as pool:
+        seqs = Sequences(pool, tables=table.cuda(), lengths=torch.tensor([L], dtype=torch.int32).cuda())
+        off = torch.tensor([0, L], dtype=torch.int32, device="cuda")
+        seqs.write(0, k, v, offsets=off)
+        pos = torch.arange(L, device="cuda")
+        where = seqs.tables[0].long()[pos // bs]
+        assert torch.equal(kv[0][where, pos % bs], k) and torch.equal(kv[1][where, pos % bs], v)
+        q = torch.randn(L, heads, dim, generator=g).to(torch.bfloat16)
+        out = seqs.attend(0, q.cuda(), offsets=off).double().cpu()
+    a = torch.einsum("ihd,jhd->hij", q.double(), data[0].double()) * dim**-0.5
+    a.masked_fill_(torch.ones(L, L).triu(1).bool(), -float("inf"))
+    p = a.softmax(-1)
+    want = torch.einsum("hij,jhd->ihd", p, data[1].double())
+    size = torch.einsum("hij,jhd->ihd", p, data[1].double().abs())
+    assert ((out - want).abs() <= 1.01 * (2.0**-8 * want.abs() + (2.0**-8 + 2.0**-14) * size)).all()
