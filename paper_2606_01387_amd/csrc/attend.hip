@@ -21,6 +21,8 @@
 // group of query heads, packed: a tile of 32 columns is filled by several
 // heads of one token, and K and V are read once for all heads of a group.
 
+#include <type_traits>
+
 #include "pool_view.h"
 
 namespace {
@@ -68,7 +70,7 @@ struct Args {
 struct Row {
   bool valid;
   uint32_t row, head;  // packed row, query head
-  int64_t limit;       // positions below it are seen
+  uint32_t limit;      // positions below it are seen
 };
 
 // Keys lo .. hi - 1 of one list of blocks.
@@ -91,24 +93,9 @@ __device__ __forceinline__ void split_pos(const Args& a, uint32_t pos, uint32_t*
   *token = r;
 }
 
-// Where position pos of the range lies: its bytes' offset in a plane, or one of
-// the two fills.
+// In place of a row's byte in a plane: nothing is there (its weight is 0), or
+// its block is missing.
 constexpr uint64_t kZeros = ~0ull, kNaNs = ~1ull;
-
-__device__ __forceinline__ uint32_t entry_of(const Args& a, const Range& g, uint32_t pos,
-                                             uint32_t* token) {
-  uint32_t at;
-  split_pos(a, pos, &at, token);
-  return pos < g.hi && at < g.entries ? g.list[at] : CLAIM_NONE;
-}
-
-__device__ __forceinline__ const uint8_t* source(const Args& a, const Range& g,
-                                                 const uint8_t* plane, uint32_t pos, uint32_t entry,
-                                                 uint32_t token, uint32_t byte, bool is_key) {
-  const uint8_t* p = plane + (uint64_t)entry * a.chunk_bytes + token * a.token_bytes + byte;
-  const uint8_t* fill = (const uint8_t*)kFill + (is_key && pos < g.hi ? 16 : 0);
-  return entry < a.nb ? p : fill;
-}
 
 // ------------------------------------------------------------ tiles in LDS
 //
@@ -127,74 +114,138 @@ __device__ __forceinline__ uint32_t v_swizzle(uint32_t row) {
   return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
 }
 
-typedef const __attribute__((address_space(1))) void* gptr;
-typedef __attribute__((address_space(3))) void* lptr;
+typedef const __attribute__((address_space(3))) u32x4 lds_words;
+
+__device__ __forceinline__ uint32_t lds_address(const uint8_t* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p;
+}
+
+// A wave's 64 lanes copy 16 bytes each to 1024 bytes of LDS from `to` (the same
+// on all lanes).  Nothing waits for it here: wait_loads() does.  (The builtin
+// makes the compiler wait for the copy at the next LDS read of any buffer.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is named so that no value is kept in it
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(from), "s"(to)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
 // Eight e4m3 bytes to eight bf16 values: every one is exact.
 __device__ __forceinline__ u32x4 widen(uint32_t a, uint32_t b) {
-  const auto pack = [](f32x2 x) {
-    return (__float_as_uint(x.x) >> 16) | (__float_as_uint(x.y) & 0xFFFF0000u);
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const auto two = [](uint32_t w, auto hi) {
+    const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, decltype(hi)::value);
+    return __builtin_bit_cast(uint32_t, x);
   };
-  return u32x4{pack(__builtin_amdgcn_cvt_pk_f32_fp8((int)a, false)),
-               pack(__builtin_amdgcn_cvt_pk_f32_fp8((int)a, true)),
-               pack(__builtin_amdgcn_cvt_pk_f32_fp8((int)b, false)),
-               pack(__builtin_amdgcn_cvt_pk_f32_fp8((int)b, true))};
+  return u32x4{two(a, std::false_type{}), two(a, std::true_type{}), two(b, std::false_type{}),
+               two(b, std::true_type{})};
 }
 
-// Moves KEYS rows of K and of V into a pair of tiles with THREADS threads.
-// bf16 rows go straight to LDS; e4m3 rows are loaded into registers by issue()
-// and widened into LDS by land().
+// Moves KEYS rows of one plane into a tile with THREADS threads.  bf16 rows go
+// straight to LDS; e4m3 rows are loaded into registers by issue() and widened
+// into LDS by land().
 template <int D, bool E4M3, int KEYS, int THREADS>
 struct Stage {
   static constexpr int kRowLanes = D * (E4M3 ? 1 : 2) / 16;  // lanes of one row
   static constexpr int kRows = THREADS / kRowLanes;          // rows of one step
   static constexpr int kSteps = KEYS / kRows ? KEYS / kRows : 1;
-  uint32_t entry[kSteps], token[kSteps];
-  u32x4 kr[E4M3 ? kSteps : 1], vr[E4M3 ? kSteps : 1];
+  static_assert(E4M3 || KEYS % kRows == 0, "bf16 tiles are filled by whole steps");
 
-  // the table entries of the tile at `pos`
-  __device__ __forceinline__ void look(const Args& a, const Range& g, uint32_t pos, uint32_t t) {
+  struct Held {  // e4m3 bytes on their way
+    u32x4 r[E4M3 ? kSteps : 1];
+  };
+
+  // This thread's rows of one tile: first where they are in the list of
+  // blocks, then, once the entries have been read, where in a plane.
+  struct Rows {
+    uint32_t at[kSteps], token[kSteps], entry[kSteps];
+  };
+  struct Places {
+    uint64_t byte[kSteps];  // kZeros, kNaNs: none
+  };
+
+  static __device__ __forceinline__ void first(const Args& a, uint32_t pos, uint32_t t, Rows& r) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      split_pos(a, pos + i * kRows + t / kRowLanes, &r.at[i], &r.token[i]);
+  }
+
+  // The rows `keys` positions on: add_blocks = keys / bs, add_tokens = keys % bs.
+  static __device__ __forceinline__ void next(const Args& a, uint32_t add_blocks, uint32_t add_tokens,
+                                              Rows& r) {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      const uint32_t row = i * kRows + t / kRowLanes;
-      entry[i] = entry_of(a, g, pos + row, &token[i]);
+      r.token[i] += add_tokens;
+      const bool over = r.token[i] >= a.bs;
+      r.token[i] = over ? r.token[i] - a.bs : r.token[i];
+      r.at[i] += add_blocks + over;
     }
   }
 
-  __device__ __forceinline__ void issue(const Args& a, const Range& g, const uint8_t* k,
-                                        const uint8_t* v, uint32_t pos, uint32_t t, uint8_t* lk,
-                                        uint8_t* lv) {
+  static __device__ __forceinline__ void look(const Range& g, Rows& r) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      r.entry[i] = CLAIM_NONE;
+      if (r.at[i] < g.entries) r.entry[i] = g.list[r.at[i]];
+    }
+  }
+
+  // `left`: how many rows of the tile are in the range.
+  static __device__ __forceinline__ Places place(const Args& a, const Rows& r, uint32_t t, uint32_t left) {
+    Places p;
+    bool lost = false;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      p.byte[i] = (uint64_t)r.entry[i] * a.chunk_bytes + r.token[i] * a.token_bytes;
+      lost |= r.entry[i] >= a.nb || i * kRows + t / kRowLanes >= left;
+    }
+    if (__any(lost)) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        if (r.entry[i] >= a.nb) p.byte[i] = kNaNs;
+        if (i * kRows + t / kRowLanes >= left) p.byte[i] = kZeros;
+      }
+    }
+    return p;
+  }
+
+  template <bool KEY>
+  static __device__ __forceinline__ void issue(const uint8_t* plane, uint32_t t, const Places& p,
+                                               uint8_t* tile, Held& held) {
+    bool lost = false;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) lost |= p.byte[i] >= kNaNs;
+    const bool any = __any(lost);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       const uint32_t row = i * kRows + t / kRowLanes, chunk = t % kRowLanes;
+      if (E4M3 && KEYS < kRows && row >= KEYS) break;
+      const uint32_t x = E4M3 ? 0 : KEY ? k_swizzle<D>(row) : v_swizzle<D>(row);
+      const uint8_t* from = plane + p.byte[i] + (chunk ^ x) * 16;
+      if (any && p.byte[i] >= kNaNs) from = (const uint8_t*)kFill + (KEY && p.byte[i] == kNaNs ? 16 : 0);
       if constexpr (E4M3) {
-        if (KEYS < kRows && row >= KEYS) break;
-        kr[i] = *(const u32x4*)source(a, g, k, pos + row, entry[i], token[i], chunk * 16, true);
-        vr[i] = *(const u32x4*)source(a, g, v, pos + row, entry[i], token[i], chunk * 16, false);
+        held.r[i] = *(const u32x4*)from;
       } else {
-        const uint8_t* ks = source(a, g, k, pos + row, entry[i], token[i],
-                                   (chunk ^ k_swizzle<D>(row)) * 16, true);
-        const uint8_t* vs = source(a, g, v, pos + row, entry[i], token[i],
-                                   (chunk ^ v_swizzle<D>(row)) * 16, false);
-        // a wave's 64 lanes fill 1024 bytes from a base of its own
-        const uint32_t at = i * THREADS * 16 + (t & ~63u) * 16;
-        __builtin_amdgcn_global_load_lds((gptr)ks, (lptr)(lk + at), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((gptr)vs, (lptr)(lv + at), 16, 0, 0);
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        copy_to_lds(from, lds_address(tile) + i * THREADS * 16 + wave * 1024);
       }
     }
   }
 
-  __device__ __forceinline__ void land(uint32_t t, uint8_t* lk, uint8_t* lv) {
+  template <bool KEY>
+  static __device__ __forceinline__ void land(uint32_t t, const Held& held, uint8_t* tile) {
     if constexpr (E4M3) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         const uint32_t row = i * kRows + t / kRowLanes, chunk = 2 * (t % kRowLanes);
         if (KEYS < kRows && row >= KEYS) break;
-        const uint32_t base = row * D * 2, xk = k_swizzle<D>(row), xv = v_swizzle<D>(row);
-        *(u32x4*)(lk + base + (chunk ^ xk) * 16) = widen(kr[i].x, kr[i].y);
-        *(u32x4*)(lk + base + ((chunk + 1) ^ xk) * 16) = widen(kr[i].z, kr[i].w);
-        *(u32x4*)(lv + base + (chunk ^ xv) * 16) = widen(vr[i].x, vr[i].y);
-        *(u32x4*)(lv + base + ((chunk + 1) ^ xv) * 16) = widen(vr[i].z, vr[i].w);
+        const uint32_t x = KEY ? k_swizzle<D>(row) : v_swizzle<D>(row);
+        uint8_t* to = tile + row * D * 2;
+        *(u32x4*)(to + (chunk ^ x) * 16) = widen(held.r[i].x, held.r[i].y);
+        *(u32x4*)(to + ((chunk + 1) ^ x) * 16) = widen(held.r[i].z, held.r[i].w);
       }
     }
   }
@@ -217,6 +268,7 @@ struct Wave {
   bf16x8 q[D / 16];
   f32x16 o[D / 32];
   float m, l;  // the maximum is the row's; the sum this lane's half of the keys
+  uint32_t k_lane, v_lane;  // this lane's place in a tile of K, of V
 
   __device__ __forceinline__ void start(const Args& a, const Row& r) {
     const uint32_t h = (threadIdx.x >> 5) & 1;
@@ -231,47 +283,53 @@ struct Wave {
     for (int j = 0; j < D / 32; ++j) o[j] = f32x16{};
     m = kNoMax;
     l = 0;
+    const uint32_t lane = threadIdx.x & 63, row = lane & 31;
+    k_lane = row * D * 2 + ((h ^ k_swizzle<D>(row)) << 4);
+    const uint32_t key = 4 * h + ((lane & 15) >> 2);
+    v_lane = key * D * 2 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D>(key)) << 4) +
+             (lane & 1) * 8;
   }
 
   // V^T's operand: 32 values of D from 32 j, keys in the order of P^T's
-  __device__ __forceinline__ bf16x8 v_operand(const uint8_t* lv, int u, int t, int j) const {
-    const uint32_t lane = threadIdx.x & 63, rr = (lane & 15) >> 2, h = lane >> 5;
-    const uint32_t row = 32 * u + 16 * t + 4 * h + rr;
-    const uint32_t chunk = (4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D>(row);
+  static __device__ __forceinline__ bf16x8 v_operand(uint32_t at, int u, int t, int j) {
     typedef __attribute__((address_space(3))) s16x4* p4;
-    const uint8_t* at = lv + row * D * 2 + chunk * 16 + (lane & 1) * 8;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)at);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(at + 8 * D * 2));
+    const uint32_t x = (at ^ (j << 6)) + (32 * u + 16 * t) * D * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)x);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)(x + 8 * D * 2));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 
-  // Adds the tile of 32 U keys at lk, lv; `first` is its first position.
-  // masked: some rows of the wave do not see all of it (the same on all lanes).
+  // Scores of a tile of 32 U keys.
   template <int U>
-  __device__ __forceinline__ void tile(const Args& a, const uint8_t* lk, const uint8_t* lv,
-                                       uint32_t first, bool masked, int64_t limit) {
-    const uint32_t lane = threadIdx.x & 63, h = lane >> 5;
-    f32x16 s[U];
+  __device__ __forceinline__ void scores(const uint8_t* lk, f32x16 (&s)[U]) const {
+    // chunk 2 t + h of row lane % 32: the swizzle leaves t an exclusive or
+    uint32_t at = lds_address(lk) + k_lane;
+    asm volatile("" : "+v"(at));  // eight exclusive ors a tile, not eight registers all along
 #pragma unroll
     for (int u = 0; u < U; ++u) s[u] = f32x16{};
 #pragma unroll
     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t row = 32 * u + (lane & 31);
-        const u32x4 w = *(const u32x4*)(lk + row * D * 2 + ((2 * t + h) ^ k_swizzle<D>(row)) * 16);
+        const u32x4 w = *(const lds_words*)(uintptr_t)((at ^ (t << 5)) + 32 * u * D * 2);
         s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), q[t], s[u], 0, 0, 0);
       }
-    int seen = 32 * U;  // keys of the tile that this lane's row sees
-    if (masked) {
-      const int64_t left = limit - first;
-      seen = left < 0 ? 0 : left > 32 * U ? 32 * U : (int)left;
+  }
+
+  // Takes out the keys past the first `seen` of the tile.
+  template <int U>
+  __device__ __forceinline__ void mask(f32x16 (&s)[U], int seen) const {
+    const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[u][r] = 32 * u + 8 * (r / 4) + r % 4 + 4 * (int)h < seen ? s[u][r] : kNoMax;
-    }
+      for (int r = 0; r < 16; ++r)
+        s[u][r] = 32 * u + 8 * (r / 4) + r % 4 < seen - 4 * h ? s[u][r] : kNoMax;
+  }
+
+  // Weights of a tile, and the running maximum and sum.
+  template <int U>
+  __device__ __forceinline__ void weights(const Args& a, const f32x16 (&s)[U], bf16x8 (&p)[U][2]) {
     float top = kNoMax;
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -290,26 +348,75 @@ struct Wave {
       m = to;
     }
     const float mc = m == kNoMax ? 0.0f : m * a.c;
-    bf16x8 p[U][2];
+    float sum[2] = {0, 0};
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c, -mc));
-        l += e;
+        sum[r & 1] += e;
         p[u][r / 8][r % 8] = (__bf16)e;
       }
-    if (masked && nonfinite<U>(lv)) {
-      by_key<U>(lv, p, seen);
-      return;
-    }
+    l += sum[0] + sum[1];
+  }
+
+  template <int U>
+  __device__ __forceinline__ void values(const uint8_t* lv, const bf16x8 (&p)[U][2]) {
+    uint32_t at = lds_address(lv) + v_lane;
+    asm volatile("" : "+v"(at));
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < D / 32; ++j)
-          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(lv, u, t, j), p[u][t], o[j], 0, 0, 0);
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(at, u, t, j), p[u][t], o[j], 0, 0, 0);
+  }
+
+  // values() of one tile of 64 keys, then scores() of another: operands are
+  // read from LDS two groups of four products ahead of their use.
+  __device__ __forceinline__ void multiply(const uint8_t* lv, const bf16x8 (&p)[2][2], const uint8_t* lk,
+                                           f32x16 (&s)[2]) {
+    values<2>(lv, p);
+    scores<2>(lk, s);
+    constexpr int kV = D / 32, kK = D / 32;  // products of a group; groups of K operands
+    constexpr int kRead = 0x100, kMul = 0x8;
+    __builtin_amdgcn_sched_group_barrier(kRead, 4 * kV, 0);
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+      }
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kRead, 4 / kV, 0);
+      }
+#pragma unroll
+    for (int g = 0; g < 4 * (kK - 2); ++g) {
+      __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMul, 8, 0);
+  }
+
+  // A whole tile of which the lane's row sees the first `seen` keys.
+  template <int U>
+  __device__ __forceinline__ void tile(const Args& a, const uint8_t* lk, const uint8_t* lv, int seen) {
+    f32x16 s[U];
+    bf16x8 p[U][2];
+    scores<U>(lk, s);
+    const bool masked = __any(seen < 32 * U);
+    if (masked) mask<U>(s, seen);
+    weights<U>(a, s, p);
+    if (masked && nonfinite<U>(lv))
+      values_seen<U>(lv, p, seen);
+    else
+      values<U>(lv, p);
   }
 
   // Whether the tile of V holds an infinity or a NaN: a weight of 0 does not
@@ -327,31 +434,40 @@ struct Wave {
     return __any(bad);
   }
 
-  // The tile's product key by key, without the keys that a row does not see.
+  // values() where V holds infinities or NaN that some rows do not see: the
+  // product over finite values, then for each place whether a row sees an
+  // infinity of either sign or a NaN there (products of ones and zeros).
   template <int U>
-  __device__ __forceinline__ void by_key(const uint8_t* lv, const bf16x8 (&p)[U][2], int seen) {
-    const uint32_t h = (threadIdx.x >> 5) & 1;
-#pragma unroll 1
-    for (int x = 0; x < 32 * U; ++x) {  // key 32 u + 8 b + 4 half + i
-      const int u = x / 32, b = x % 32 / 8, half = x % 8 / 4, i = x % 4;
-      float w = 0;
+  __device__ __forceinline__ void values_seen(const uint8_t* lv, const bf16x8 (&p)[U][2], int seen) {
+    const int h = (threadIdx.x >> 5) & 1;
+    const uint32_t at = lds_address(lv) + v_lane;
+    const __bf16 zero = (__bf16)0.0f, one = (__bf16)1.0f;
 #pragma unroll
-      for (int y = 0; y < 16 * U; ++y)
-        if (y == u * 16 + b * 4 + i) w = (float)p[y / 16][y / 8 % 2][y % 8];
-      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
-      w = __uint_as_float(half ? both[1] : both[0]);
+    for (int j = 0; j < D / 32; ++j) {
+      f32x16 up = {}, down = {};  // infinities seen; a NaN counts as both
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const uint32_t d = 32 * j + 8 * g + 4 * h;
-          const u32x2 v = *(const u32x2*)(lv + x * D * 2 + ((d / 8) ^ v_swizzle<D>(x)) * 16 + d % 8 * 2);
+        for (int t = 0; t < 2; ++t) {
+          const bf16x8 v = v_operand(at, u, t, j);
+          bf16x8 fine, high, low, sees;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float e = __uint_as_float(r & 1 ? v[r / 2] & 0xFFFF0000u : v[r / 2] << 16);
-            o[j][4 * g + r] = x < seen ? __builtin_fmaf(w, e, o[j][4 * g + r]) : o[j][4 * g + r];
+          for (int i = 0; i < 8; ++i) {
+            const uint16_t w = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+            fine[i] = (w & 0x7F80) == 0x7F80 ? zero : v[i];
+            high[i] = (w & 0x7F80) == 0x7F80 && w != 0xFF80 ? one : zero;
+            low[i] = (w & 0x7F80) == 0x7F80 && w != 0x7F80 ? one : zero;
+            sees[i] = 32 * u + 16 * t + 8 * (i / 4) + i % 4 < seen - 4 * h ? one : zero;
           }
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fine, p[u][t], o[j], 0, 0, 0);
+          up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(high, sees, up, 0, 0, 0);
+          down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(low, sees, down, 0, 0, 0);
         }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (up[r] > 0) o[j][r] += __builtin_inff();
+        if (down[r] > 0) o[j][r] -= __builtin_inff();
+      }
     }
   }
 
@@ -415,7 +531,7 @@ struct Item {
   Row row;
   Range range;
   uint32_t wave_hi;  // positions at or past it are seen by no row of the wave
-  int64_t all_below; // every valid row of the wave sees the positions below it
+  uint32_t all_below;  // every valid row of the wave sees the positions below it
   uint32_t split;
   bool any;          // the item has rows
 };
@@ -424,8 +540,7 @@ struct Item {
 // split.
 template <int M>
 __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t tile, uint32_t split,
-                                          uint32_t kv_head, uint32_t r, uint32_t wave_first,
-                                          uint32_t align) {
+                                          uint32_t kv_head, uint32_t r, uint32_t align) {
   Item it;
   it.row.valid = false;
   it.row.row = it.row.head = 0;
@@ -454,7 +569,7 @@ __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t t
       it.row.row = row;
       it.row.head = kv_head * a.group + (uint32_t)(x % a.group);
       const int64_t limit = id < a.max_seqs ? (int64_t)a.lengths[id] - n + i + 1 : 0;
-      it.row.limit = limit < a.prefix_tokens ? limit : a.prefix_tokens;
+      it.row.limit = (uint32_t)(limit < 0 ? 0 : limit < a.prefix_tokens ? limit : a.prefix_tokens);
     }
     it.range = Range{a.prefix, a.prefix_tokens / a.bs, 0, a.prefix_tokens};
     splits = a.prefix_splits;
@@ -475,7 +590,7 @@ __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t t
       it.row.valid = true;
       it.row.row = first + i;
       it.row.head = kv_head * a.group + (uint32_t)(x % a.group);
-      it.row.limit = len - n + i + 1;
+      it.row.limit = len - n + i + 1 > 0 ? (uint32_t)(len - n + i + 1) : 0;
     }
     const uint64_t last = x0 + M < all ? x0 + M : all;
     top = it.any ? len - n + (int64_t)((last + a.group - 1) / a.group) : 0;
@@ -499,18 +614,21 @@ __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t t
   it.range.lo = (uint32_t)(lo + from);
   it.range.hi = (uint32_t)(lo + to);
   // per wave: the most and the least that a row sees
-  const int64_t big = it.row.valid ? it.row.limit : 0;
-  const int64_t small = it.row.valid ? it.row.limit : INT64_MAX;
-  int64_t hi = big, least = small;
+  uint32_t most = it.row.valid ? it.row.limit : 0, least = it.row.valid ? it.row.limit : ~0u;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t b = __shfl_xor(hi, d), s2 = __shfl_xor(least, d);
-    hi = b > hi ? b : hi;
-    least = s2 < least ? s2 : least;
+    const uint32_t x = __shfl_xor(most, d), y = __shfl_xor(least, d);
+    most = x > most ? x : most;
+    least = y < least ? y : least;
   }
-  it.wave_hi = hi < 0 ? 0 : (uint32_t)(hi < it.range.hi ? hi : it.range.hi);
+  it.wave_hi = most;
   it.all_below = least;
   return it;
+}
+
+// How many of the `keys` positions from `pos` on the row sees.
+__device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys) {
+  return r.limit <= pos ? 0 : r.limit - pos < keys ? (int)(r.limit - pos) : (int)keys;
 }
 
 // Everything that this wave has asked memory for has arrived.
@@ -528,13 +646,22 @@ __device__ __forceinline__ void meet() {
 
 // ----------------------------------------------------------- many query rows
 //
-// WAVES waves of 32 rows share each tile of 64 keys.  Two pairs of tiles: one
-// is filled while the other is read.
+// WAVES waves of 32 rows share each tile of 64 keys.  The tiles that every row
+// sees in full take two phases each: a wave multiplies (the weights of the
+// tile before with V, then the queries with K), then it turns the scores into
+// weights.  Half of the waves, one on each SIMD, are one phase ahead of their
+// partners on the SIMDs, so matrix cores and vector units are both busy all
+// the time.  Three tiles of K and three of V: two phases after its copy
+// began, a tile is there.  The tiles that some row does not see in full come
+// last, one after another.
 
 template <int D, bool E4M3, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
   constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2;
-  __shared__ __align__(1024) uint8_t lds[2][2][kTile];
+  using St = Stage<D, E4M3, kKeys, WAVES * 64>;
+  __shared__ __align__(1024) uint8_t lk[3 * kTile];
+  __shared__ __align__(1024) uint8_t lv[3 * kTile];
+  __shared__ uint32_t least[WAVES];
   const uint32_t t = threadIdx.x;
   uint32_t b = blockIdx.x;
   const uint32_t kv_head = b % a.heads;  // one head's keys stay in one die's cache where heads = 8
@@ -543,36 +670,109 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   const uint32_t split = b % splits, tiles = prefix ? a.prefix_tiles : a.tiles;
   const uint32_t tile = tiles - 1 - b / splits;  // late rows see the most: they start first
   const uint32_t r = (t >> 6) * 32 + (t & 31);
-  const Item it = make_item<M>(a, prefix, tile, split, kv_head, r, 0, kKeys);
+  const Item it = make_item<M>(a, prefix, tile, split, kv_head, r, kKeys);
   if (!it.any) return;
   const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
+  const uint32_t lo = it.range.lo, hi = it.range.hi;
+  // whole tiles that every row of the workgroup sees
+  if ((t & 63) == 0) least[t >> 6] = it.all_below;
+  __syncthreads();
+  uint32_t below = hi;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) below = least[w] < below ? least[w] : below;
+  const uint32_t full = __builtin_amdgcn_readfirstlane(below > lo ? (below - lo) / kKeys : 0);
+
   Wave<D> w;
   w.start(a, it.row);
-  Stage<D, E4M3, kKeys, WAVES * 64> st;
-  const uint32_t lo = it.range.lo, hi = it.range.hi;
-  if (lo < hi) {
-    st.look(a, it.range, lo, t);
-    st.issue(a, it.range, k, v, lo, t, lds[0][0], lds[0][1]);
-    st.land(t, lds[0][0], lds[0][1]);
-    st.look(a, it.range, lo + kKeys, t);
+  typename St::Held kh, vh;
+  if (full) {
+    const uint32_t add_blocks = kKeys / a.bs, add_tokens = kKeys % a.bs;
+    typename St::Rows rows;
+    St::first(a, lo, t, rows);
+    St::look(it.range, rows);
+    typename St::Places kp = St::place(a, rows, t, kKeys), vp = kp;
+    St::template issue<true>(k, t, kp, lk, kh);
+    St::template issue<false>(v, t, vp, lv, vh);
+    St::template land<true>(t, kh, lk);
+    St::template land<false>(t, vh, lv);
+    St::next(a, add_blocks, add_tokens, rows);
+    St::look(it.range, rows);
+    vp = kp = St::place(a, rows, t, kKeys);  // keys past the full tiles are copied too: nothing reads them
+    St::template issue<true>(k, t, kp, lk + kTile, kh);
+    St::template land<true>(t, kh, lk + kTile);
+    St::next(a, add_blocks, add_tokens, rows);
+    St::look(it.range, rows);
     wait_loads();
     meet();
-  }
-  int at = 0;
-  for (uint32_t pos = lo; pos < hi; pos += kKeys, at ^= 1) {  // hi + kKeys fits 32 bits
-    const bool more = pos + kKeys < hi;
-    if (more) st.issue(a, it.range, k, v, pos + kKeys, t, lds[at ^ 1][0], lds[at ^ 1][1]);
-    if (pos < it.wave_hi) {
-      w.template tile<2>(a, lds[at][0], lds[at][1], pos, (int64_t)pos + kKeys > it.all_below,
-                         it.row.limit);
-    }
-    if (more) {
-      st.land(t, lds[at ^ 1][0], lds[at ^ 1][1]);
-      st.look(a, it.range, pos + 2 * kKeys, t);
+    if (__builtin_amdgcn_readfirstlane(t >> 6) >= WAVES / 2) meet();  // these waves are a phase behind
+    f32x16 s[2];
+    bf16x8 p[2][2];
+    uint32_t k0 = 0, k2 = 2 * kTile, v0 = 2 * kTile, v1 = kTile;  // tiles n, n + 2 of K; n - 1, n + 1 of V
+    const auto fetch = [&] {
+      kp = St::place(a, rows, t, kKeys);
+      St::template issue<true>(k, t, kp, lk + k2, kh);
+      St::template issue<false>(v, t, vp, lv + v1, vh);
+      vp = kp;
+      St::next(a, add_blocks, add_tokens, rows);
+      St::look(it.range, rows);
+    };
+    const auto change = [&] {
+      meet();
+      w.template weights<2>(a, s, p);
+      St::template land<true>(t, kh, lk + k2);
+      St::template land<false>(t, vh, lv + v1);
+      const uint32_t kt = k2, vt = v1;
+      k2 = k0;  // tile n + 3 takes the place of tile n
+      k0 = kTile * 3 - k2 - kt;
+      v1 = v0;
+      v0 = kTile * 3 - v1 - vt;
       wait_loads();
+      meet();
+    };
+    fetch();
+    w.template scores<2>(lk + k0, s);
+    change();
+#pragma unroll 1
+    for (uint32_t n = 1; n < full; ++n) {
+      fetch();
+      __builtin_amdgcn_s_setprio(1);
+      w.multiply(lv + v0, p, lk + k0, s);
+      __builtin_amdgcn_s_setprio(0);
+      change();
     }
+    w.template values<2>(lv + v0, p);
+    if (__builtin_amdgcn_readfirstlane(t >> 6) < WAVES / 2) meet();
     meet();
+  }
+  uint32_t pos = lo + full * kKeys;
+  if (pos < hi) {
+    typename St::Rows rows;
+    const auto fetch = [&](uint32_t from, uint32_t buffer) {
+      St::first(a, from, t, rows);
+      St::look(it.range, rows);
+      const typename St::Places at = St::place(a, rows, t, hi - from);
+      St::template issue<true>(k, t, at, lk + buffer, kh);
+      St::template issue<false>(v, t, at, lv + buffer, vh);
+    };
+    fetch(pos, 0);
+    St::template land<true>(t, kh, lk);
+    St::template land<false>(t, vh, lv);
+    wait_loads();
+    meet();
+    uint32_t at = 0;
+#pragma unroll 1
+    for (; pos < hi; pos += kKeys, at ^= kTile) {  // hi + kKeys fits 32 bits
+      const bool more = pos + kKeys < hi;
+      if (more) fetch(pos + kKeys, at ^ kTile);
+      if (pos < it.wave_hi) w.template tile<2>(a, lk + at, lv + at, seen_of(it.row, pos, kKeys));
+      if (more) {
+        St::template land<true>(t, kh, lk + (at ^ kTile));
+        St::template land<false>(t, vh, lv + (at ^ kTile));
+      }
+      wait_loads();
+      meet();
+    }
   }
   w.finish(a, it.row, a.part_o != nullptr, it.split, a.own_splits + a.prefix_splits);
 }
@@ -586,41 +786,54 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(256, 1) k_attend_few(Args a) {
   constexpr int M = 32, kKeys = 32, kTile = kKeys * D * 2, kWaves = 4;
+  using St = Stage<D, E4M3, kKeys, 64>;
   __shared__ __align__(1024) uint8_t lds[kWaves][2][2][kTile];
-  const uint32_t wave = threadIdx.x >> 6, t = threadIdx.x & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = threadIdx.x & 63;
   uint32_t b = blockIdx.x;
   const uint32_t kv_head = b % a.heads;
   b /= a.heads;
   const uint32_t split = b % a.own_splits, tile = b / a.own_splits;
-  const Item it = make_item<M>(a, false, tile, split, kv_head, t & 31, 0, kKeys);
+  const Item it = make_item<M>(a, false, tile, split, kv_head, t & 31, kKeys);
   if (!it.any) return;
   const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
   Wave<D> w;
   w.start(a, it.row);
-  Stage<D, E4M3, kKeys, 64> st;
   // tiles wave, wave + 4, ... of the range
-  const uint32_t hi = it.range.hi, lo = it.range.lo + wave * kKeys;
+  constexpr uint32_t kStep = kWaves * kKeys;
+  const uint32_t hi = it.range.hi;
+  uint32_t pos = it.range.lo + wave * kKeys;
   uint8_t(*mine)[2][kTile] = lds[wave];
-  if (lo < hi) {
-    st.look(a, it.range, lo, t);
-    st.issue(a, it.range, k, v, lo, t, mine[0][0], mine[0][1]);
-    st.land(t, mine[0][0], mine[0][1]);
-    st.look(a, it.range, lo + kWaves * kKeys, t);
+  typename St::Held kh, vh;
+  if (pos < hi) {
+    const uint32_t add_blocks = kStep / a.bs, add_tokens = kStep % a.bs;
+    typename St::Rows rows;
+    St::first(a, pos, t, rows);
+    St::look(it.range, rows);
+    typename St::Places at = St::place(a, rows, t, hi - pos);
+    St::template issue<true>(k, t, at, mine[0][0], kh);
+    St::template issue<false>(v, t, at, mine[0][1], vh);
+    St::template land<true>(t, kh, mine[0][0]);
+    St::template land<false>(t, vh, mine[0][1]);
+    St::next(a, add_blocks, add_tokens, rows);
+    St::look(it.range, rows);
     wait_loads();
-  }
-  int at = 0;
-  for (uint64_t p64 = lo; p64 < hi; p64 += kWaves * kKeys, at ^= 1) {
-    const uint32_t pos = (uint32_t)p64;
-    const bool more = p64 + kWaves * kKeys < hi;
-    if (more) st.issue(a, it.range, k, v, pos + kWaves * kKeys, t, mine[at ^ 1][0], mine[at ^ 1][1]);
-    if (pos < it.wave_hi) {
-      w.template tile<1>(a, mine[at][0], mine[at][1], pos, (int64_t)pos + kKeys > it.all_below,
-                         it.row.limit);
-    }
-    if (more) {
-      st.land(t, mine[at ^ 1][0], mine[at ^ 1][1]);
-      st.look(a, it.range, pos + 2 * kWaves * kKeys, t);
+    int x = 0;
+#pragma unroll 1
+    for (; pos < hi; pos += kStep, x ^= 1) {  // hi + kStep fits 32 bits
+      const bool more = pos + kStep < hi;
+      if (more) {
+        at = St::place(a, rows, t, hi - pos - kStep);
+        St::template issue<true>(k, t, at, mine[x ^ 1][0], kh);
+        St::template issue<false>(v, t, at, mine[x ^ 1][1], vh);
+        St::next(a, add_blocks, add_tokens, rows);
+        St::look(it.range, rows);
+      }
+      if (pos < it.wave_hi) w.template tile<1>(a, mine[x][0], mine[x][1], seen_of(it.row, pos, kKeys));
+      if (more) {
+        St::template land<true>(t, kh, mine[x ^ 1][0]);
+        St::template land<false>(t, vh, mine[x ^ 1][1]);
+      }
       wait_loads();
     }
   }
