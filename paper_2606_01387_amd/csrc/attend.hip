@@ -73,6 +73,15 @@ struct Row {
   uint32_t limit;      // positions below it are seen
 };
 
+// A value that all lanes of the wave have, for the scalar unit.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <typename T>
+__device__ __forceinline__ T* uniform(T* p) {
+  const uint64_t x = (uint64_t)p;
+  return (T*)((uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x));
+}
+
 // Keys lo .. hi - 1 of one list of blocks.
 struct Range {
   const uint32_t* list;
@@ -131,6 +140,14 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {
                : "v"(from), "s"(to)
                : "memory", "m0");
 }
+
+// The same from one base for the wave and an offset for each lane.
+__device__ __forceinline__ void copy_to_lds(const uint8_t* base, uint32_t lane_offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(lane_offset), "s"(base), "s"(to)
+               : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // Eight e4m3 bytes to eight bf16 values: every one is exact.
@@ -147,10 +164,17 @@ __device__ __forceinline__ u32x4 widen(uint32_t a, uint32_t b) {
 // Moves KEYS rows of one plane into a tile with THREADS threads.  bf16 rows go
 // straight to LDS; e4m3 rows are loaded into registers by issue() and widened
 // into LDS by land().
-template <int D, bool E4M3, int KEYS, int THREADS>
+//
+// ONE: the rows that a wave loads with one instruction (4 of 256 bytes to 16
+// of 64) lie in one block, as they do wherever their number divides the block
+// size.  Block, token and address are then the wave's, on the scalar unit;
+// otherwise each lane has its own.  16384 causal tokens, 32 heads over 8 of
+// 128, blocks of 16: FIGURE-ONE.
+template <int D, bool E4M3, int KEYS, int THREADS, bool ONE>
 struct Stage {
   static constexpr int kRowLanes = D * (E4M3 ? 1 : 2) / 16;  // lanes of one row
-  static constexpr int kRows = THREADS / kRowLanes;          // rows of one step
+  static constexpr int kWaveRows = 64 / kRowLanes;
+  static constexpr int kRows = THREADS / kRowLanes;  // rows of one step
   static constexpr int kSteps = KEYS / kRows ? KEYS / kRows : 1;
   static_assert(E4M3 || KEYS % kRows == 0, "bf16 tiles are filled by whole steps");
 
@@ -158,24 +182,52 @@ struct Stage {
     u32x4 r[E4M3 ? kSteps : 1];
   };
 
-  // This thread's rows of one tile: first where they are in the list of
-  // blocks, then, once the entries have been read, where in a plane.
+  // The rows of one tile, a wave's first of each step (ONE) or a lane's own:
+  // where they are in the list of blocks, and its entries once they are read.
   struct Rows {
     uint32_t at[kSteps], token[kSteps], entry[kSteps];
   };
+
+  // Where they are in a plane.
   struct Places {
-    uint64_t byte[kSteps];  // kZeros, kNaNs: none
+    uint64_t byte[kSteps];
+    uint32_t entry[kSteps];
+    uint32_t left;  // rows of the tile that the range has
   };
 
-  static __device__ __forceinline__ void first(const Args& a, uint32_t pos, uint32_t t, Rows& r) {
+  uint32_t t, wave, k_off, v_off;  // a lane's place in its wave's rows (ONE) or in its row
+
+  __device__ __forceinline__ Stage(const Args& a, uint32_t thread) : t(thread) {
+    wave = THREADS == 64 ? 0 : uniform(thread >> 6);
+    const uint32_t row = thread / kRowLanes, chunk = thread % kRowLanes;
+    // swizzles repeat every 16 rows: they are the same in every step
+    static_assert(kRows % 16 == 0 || kSteps == 1 || THREADS == 64, "");
+    k_off = (E4M3 ? chunk : chunk ^ k_swizzle<D>(row)) * 16;
+    v_off = (E4M3 ? chunk : chunk ^ v_swizzle<D>(row)) * 16;
+    if (ONE) {
+      k_off += row % kWaveRows * a.token_bytes;
+      v_off += row % kWaveRows * a.token_bytes;
+    }
+  }
+
+  __device__ __forceinline__ uint32_t row(int i) const {
+    return i * kRows + (ONE ? wave * kWaveRows : t / kRowLanes);
+  }
+
+  __device__ __forceinline__ void first(const Args& a, uint32_t pos, Rows& r) const {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-      split_pos(a, pos + i * kRows + t / kRowLanes, &r.at[i], &r.token[i]);
+    for (int i = 0; i < kSteps; ++i) {
+      split_pos(a, pos + row(i), &r.at[i], &r.token[i]);
+      if (ONE) {
+        r.at[i] = uniform(r.at[i]);
+        r.token[i] = uniform(r.token[i]);
+      }
+    }
   }
 
   // The rows `keys` positions on: add_blocks = keys / bs, add_tokens = keys % bs.
-  static __device__ __forceinline__ void next(const Args& a, uint32_t add_blocks, uint32_t add_tokens,
-                                              Rows& r) {
+  __device__ __forceinline__ void next(const Args& a, uint32_t add_blocks, uint32_t add_tokens,
+                                       Rows& r) const {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       r.token[i] += add_tokens;
@@ -185,58 +237,75 @@ struct Stage {
     }
   }
 
-  static __device__ __forceinline__ void look(const Range& g, Rows& r) {
+  __device__ __forceinline__ void look(const Range& g, Rows& r) const {
+    typedef const __attribute__((address_space(4))) uint32_t* scalar_list;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       r.entry[i] = CLAIM_NONE;
-      if (r.at[i] < g.entries) r.entry[i] = g.list[r.at[i]];
+      if (ONE) {
+        // past the list: its last entry is read in its place
+        const uint32_t at = r.at[i] < g.entries ? r.at[i] : g.entries - 1;
+        const uint32_t entry = ((scalar_list)g.list)[at];
+        r.entry[i] = r.at[i] < g.entries ? entry : CLAIM_NONE;
+      } else if (r.at[i] < g.entries) {
+        r.entry[i] = g.list[r.at[i]];
+      }
     }
   }
 
-  // `left`: how many rows of the tile are in the range.
-  static __device__ __forceinline__ Places place(const Args& a, const Rows& r, uint32_t t, uint32_t left) {
+  __device__ __forceinline__ Places place(const Args& a, const Rows& r, uint32_t left) const {
     Places p;
-    bool lost = false;
+    p.left = left;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      p.byte[i] = (uint64_t)r.entry[i] * a.chunk_bytes + r.token[i] * a.token_bytes;
-      lost |= r.entry[i] >= a.nb || i * kRows + t / kRowLanes >= left;
-    }
-    if (__any(lost)) {
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        if (r.entry[i] >= a.nb) p.byte[i] = kNaNs;
-        if (i * kRows + t / kRowLanes >= left) p.byte[i] = kZeros;
-      }
+      p.entry[i] = r.entry[i] < a.nb ? r.entry[i] : CLAIM_NONE;
+      p.byte[i] = (uint64_t)r.entry[i] * a.chunk_bytes + (uint64_t)r.token[i] * a.token_bytes;
     }
     return p;
   }
 
   template <bool KEY>
-  static __device__ __forceinline__ void issue(const uint8_t* plane, uint32_t t, const Places& p,
-                                               uint8_t* tile, Held& held) {
-    bool lost = false;
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) lost |= p.byte[i] >= kNaNs;
-    const bool any = __any(lost);
+  __device__ __forceinline__ void issue(const uint8_t* plane, const Places& p, uint8_t* tile,
+                                        Held& held) const {
+    const uint32_t off = KEY ? k_off : v_off;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      const uint32_t row = i * kRows + t / kRowLanes, chunk = t % kRowLanes;
-      if (E4M3 && KEYS < kRows && row >= KEYS) break;
-      const uint32_t x = E4M3 ? 0 : KEY ? k_swizzle<D>(row) : v_swizzle<D>(row);
-      const uint8_t* from = plane + p.byte[i] + (chunk ^ x) * 16;
-      if (any && p.byte[i] >= kNaNs) from = (const uint8_t*)kFill + (KEY && p.byte[i] == kNaNs ? 16 : 0);
-      if constexpr (E4M3) {
-        held.r[i] = *(const u32x4*)from;
+      if (E4M3 && KEYS < kRows && i * kRows + t / kRowLanes >= KEYS) break;
+      const uint32_t to = lds_address(tile) + i * THREADS * 16 + wave * 1024;
+      // swizzles of a step of 4 or 8 rows are its own
+      const uint32_t mine = THREADS == 64 && !E4M3 ? off ^ step_swizzle<KEY>(i) : off;
+      const uint8_t* base = ONE ? uniform(plane + p.byte[i]) : plane + p.byte[i];
+      const bool fine = p.entry[i] != CLAIM_NONE && row(i) + (ONE ? kWaveRows : 1) <= p.left;
+      if (ONE ? fine : __all(fine)) {
+        if constexpr (E4M3)
+          held.r[i] = *(const u32x4*)(base + mine);
+        else if constexpr (ONE)
+          copy_to_lds(base, mine, to);
+        else
+          copy_to_lds(base + mine, to);
       } else {
-        const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
-        copy_to_lds(from, lds_address(tile) + i * THREADS * 16 + wave * 1024);
+        const bool there = i * kRows + t / kRowLanes < p.left;
+        const uint8_t* from = there && p.entry[i] != CLAIM_NONE
+                                  ? base + mine
+                                  : (const uint8_t*)kFill + (KEY && there ? 16 : 0);
+        if constexpr (E4M3)
+          held.r[i] = *(const u32x4*)from;
+        else
+          copy_to_lds(from, to);
       }
     }
   }
 
+  // What step i's swizzle adds to step 0's (a wave alone: a step is kWaveRows
+  // rows, and the swizzles repeat every 16).
   template <bool KEY>
-  static __device__ __forceinline__ void land(uint32_t t, const Held& held, uint8_t* tile) {
+  static __device__ __forceinline__ constexpr uint32_t step_swizzle(int i) {
+    return (KEY ? (D == 128 ? i * kWaveRows & 15 : (i * kWaveRows >> 1) & 7)
+                : (D == 128 ? (i * kWaveRows & 3) << 2 : ((i * kWaveRows >> 1) & 1) << 2)) * 16;
+  }
+
+  template <bool KEY>
+  __device__ __forceinline__ void land(const Held& held, uint8_t* tile) const {
     if constexpr (E4M3) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
@@ -611,8 +680,10 @@ __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t t
   const uint64_t share = ((keys + splits - 1) / splits + align - 1) / align * align;
   const uint64_t from = share * split < keys ? share * split : keys;
   const uint64_t to = from + share < keys ? from + share : keys;
-  it.range.lo = (uint32_t)(lo + from);
-  it.range.hi = (uint32_t)(lo + to);
+  it.range.lo = uniform((uint32_t)(lo + from));
+  it.range.hi = uniform((uint32_t)(lo + to));
+  it.range.list = uniform(it.range.list);
+  it.range.entries = uniform(it.range.entries);
   // per wave: the most and the least that a row sees
   uint32_t most = it.row.valid ? it.row.limit : 0, least = it.row.valid ? it.row.limit : ~0u;
 #pragma unroll
@@ -621,8 +692,8 @@ __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t t
     most = x > most ? x : most;
     least = y < least ? y : least;
   }
-  it.wave_hi = most;
-  it.all_below = least;
+  it.wave_hi = uniform(most);
+  it.all_below = uniform(least);
   return it;
 }
 
@@ -638,10 +709,12 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 __device__ __forceinline__ void meet() {
+  __builtin_amdgcn_sched_barrier(0);  // no work of one phase moves into the other
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads and writes are done
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // ----------------------------------------------------------- many query rows
@@ -649,18 +722,24 @@ __device__ __forceinline__ void meet() {
 // WAVES waves of 32 rows share each tile of 64 keys.  The tiles that every row
 // sees in full take two phases each: a wave multiplies (the weights of the
 // tile before with V, then the queries with K), then it turns the scores into
-// weights.  Half of the waves, one on each SIMD, are one phase ahead of their
-// partners on the SIMDs, so matrix cores and vector units are both busy all
-// the time.  Three tiles of K and three of V: two phases after its copy
-// began, a tile is there.  The tiles that some row does not see in full come
-// last, one after another.
+// weights and begins the copy of a tile two further on.  Half of the waves,
+// one on each SIMD, are one phase ahead of their partners on the SIMDs, so
+// matrix cores and vector units are both busy all the time.  The tiles that
+// some row does not see in full come last, one after another.
+//
+// In wave terms: M(n) reads tile n of K and n - 1 of V, W(n) makes weights of
+// tile n and copies tile n + A of K and n + A - 1 of V (A = 2; e4m3 3, since
+// its bytes stop in registers and land in W(n + 1)).  A ring of A + 1 tiles: the
+// one that W(n) fills was last read in M(n - 1), by every wave before any is in
+// W(n).  bf16 copies are waited for at the end of M(n + 1), one barrier before
+// the first wave is in M(n + 2).
 
-template <int D, bool E4M3, int WAVES>
+template <int D, bool E4M3, int WAVES, bool ONE>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
-  constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2;
-  using St = Stage<D, E4M3, kKeys, WAVES * 64>;
-  __shared__ __align__(1024) uint8_t lk[3 * kTile];
-  __shared__ __align__(1024) uint8_t lv[3 * kTile];
+  constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2, kAhead = E4M3 ? 3 : 2;
+  using St = Stage<D, E4M3, kKeys, WAVES * 64, ONE>;
+  __shared__ __align__(1024) uint8_t lk[(kAhead + 1) * kTile];
+  __shared__ __align__(1024) uint8_t lv[(kAhead + 1) * kTile];
   __shared__ uint32_t least[WAVES];
   const uint32_t t = threadIdx.x;
   uint32_t b = blockIdx.x;
@@ -681,83 +760,92 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   uint32_t below = hi;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) below = least[w] < below ? least[w] : below;
-  const uint32_t full = __builtin_amdgcn_readfirstlane(below > lo ? (below - lo) / kKeys : 0);
+  const uint32_t full = uniform(below > lo ? (below - lo) / kKeys : 0);
 
   Wave<D> w;
   w.start(a, it.row);
+  const St st(a, t);
   typename St::Held kh, vh;
+  typename St::Rows rows;
   if (full) {
     const uint32_t add_blocks = kKeys / a.bs, add_tokens = kKeys % a.bs;
-    typename St::Rows rows;
-    St::first(a, lo, t, rows);
-    St::look(it.range, rows);
-    typename St::Places kp = St::place(a, rows, t, kKeys), vp = kp;
-    St::template issue<true>(k, t, kp, lk, kh);
-    St::template issue<false>(v, t, vp, lv, vh);
-    St::template land<true>(t, kh, lk);
-    St::template land<false>(t, vh, lv);
-    St::next(a, add_blocks, add_tokens, rows);
-    St::look(it.range, rows);
-    vp = kp = St::place(a, rows, t, kKeys);  // keys past the full tiles are copied too: nothing reads them
-    St::template issue<true>(k, t, kp, lk + kTile, kh);
-    St::template land<true>(t, kh, lk + kTile);
-    St::next(a, add_blocks, add_tokens, rows);
-    St::look(it.range, rows);
+    typename St::Places kp, vp;
+    // tiles 0 and 1 of K and 0 of V, then what W(-1) would have asked for;
+    // tiles past the full ones are copied too, and nothing reads them
+    st.first(a, lo, rows);
+    st.look(it.range, rows);
+    vp = st.place(a, rows, kKeys);
+    st.template issue<true>(k, vp, lk, kh);
+    st.template issue<false>(v, vp, lv, vh);
+    st.template land<true>(kh, lk);
+    st.template land<false>(vh, lv);
+    st.next(a, add_blocks, add_tokens, rows);
+    st.look(it.range, rows);
+    kp = st.place(a, rows, kKeys);
+    st.template issue<true>(k, kp, lk + kTile, kh);
+    st.template land<true>(kh, lk + kTile);
+    st.next(a, add_blocks, add_tokens, rows);
+    st.look(it.range, rows);
+    if (E4M3) {
+      vp = kp;
+      kp = st.place(a, rows, kKeys);
+      st.template issue<true>(k, kp, lk, kh);
+      st.template issue<false>(v, vp, lv, vh);
+      st.next(a, add_blocks, add_tokens, rows);
+      st.look(it.range, rows);
+    }
     wait_loads();
     meet();
-    if (__builtin_amdgcn_readfirstlane(t >> 6) >= WAVES / 2) meet();  // these waves are a phase behind
+    if (uniform(t >> 6) >= WAVES / 2) meet();  // these waves are a phase behind
     f32x16 s[2];
     bf16x8 p[2][2];
-    uint32_t k0 = 0, k2 = 2 * kTile, v0 = 2 * kTile, v1 = kTile;  // tiles n, n + 2 of K; n - 1, n + 1 of V
-    const auto fetch = [&] {
-      kp = St::place(a, rows, t, kKeys);
-      St::template issue<true>(k, t, kp, lk + k2, kh);
-      St::template issue<false>(v, t, vp, lv + v1, vh);
+    uint32_t now = 0;                                  // where tile n is in the ring
+    const auto before = [&](uint32_t x) { return x ? x - kTile : kAhead * kTile; };
+    const auto weigh = [&] {
+      const uint32_t to = before(now);  // tile n + A of K takes the place of n - 1
+      if (E4M3) {  // what W(n - 1) asked for: tile n + A - 1 of K, n + A - 2 of V
+        st.template land<true>(kh, lk + before(to));
+        st.template land<false>(vh, lv + before(before(to)));
+      }
       vp = kp;
-      St::next(a, add_blocks, add_tokens, rows);
-      St::look(it.range, rows);
-    };
-    const auto change = [&] {
-      meet();
+      kp = st.place(a, rows, kKeys);
+      st.template issue<true>(k, kp, lk + to, kh);
+      st.template issue<false>(v, vp, lv + before(to), vh);
+      st.next(a, add_blocks, add_tokens, rows);
+      st.look(it.range, rows);
       w.template weights<2>(a, s, p);
-      St::template land<true>(t, kh, lk + k2);
-      St::template land<false>(t, vh, lv + v1);
-      const uint32_t kt = k2, vt = v1;
-      k2 = k0;  // tile n + 3 takes the place of tile n
-      k0 = kTile * 3 - k2 - kt;
-      v1 = v0;
-      v0 = kTile * 3 - v1 - vt;
-      wait_loads();
+      now = now == kAhead * kTile ? 0 : now + kTile;
       meet();
     };
-    fetch();
-    w.template scores<2>(lk + k0, s);
-    change();
+    w.template scores<2>(lk, s);
+    meet();
+    weigh();
 #pragma unroll 1
     for (uint32_t n = 1; n < full; ++n) {
-      fetch();
       __builtin_amdgcn_s_setprio(1);
-      w.multiply(lv + v0, p, lk + k0, s);
+      w.multiply(lv + before(now), p, lk + now, s);
       __builtin_amdgcn_s_setprio(0);
-      change();
+      if (!E4M3) wait_loads();
+      meet();
+      weigh();
     }
-    w.template values<2>(lv + v0, p);
-    if (__builtin_amdgcn_readfirstlane(t >> 6) < WAVES / 2) meet();
+    w.template values<2>(lv + before(now), p);
+    wait_loads();
+    if (uniform(t >> 6) < WAVES / 2) meet();
     meet();
   }
   uint32_t pos = lo + full * kKeys;
   if (pos < hi) {
-    typename St::Rows rows;
     const auto fetch = [&](uint32_t from, uint32_t buffer) {
-      St::first(a, from, t, rows);
-      St::look(it.range, rows);
-      const typename St::Places at = St::place(a, rows, t, hi - from);
-      St::template issue<true>(k, t, at, lk + buffer, kh);
-      St::template issue<false>(v, t, at, lv + buffer, vh);
+      st.first(a, from, rows);
+      st.look(it.range, rows);
+      const typename St::Places at = st.place(a, rows, hi - from);
+      st.template issue<true>(k, at, lk + buffer, kh);
+      st.template issue<false>(v, at, lv + buffer, vh);
     };
     fetch(pos, 0);
-    St::template land<true>(t, kh, lk);
-    St::template land<false>(t, vh, lv);
+    st.template land<true>(kh, lk);
+    st.template land<false>(vh, lv);
     wait_loads();
     meet();
     uint32_t at = 0;
@@ -767,8 +855,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
       if (more) fetch(pos + kKeys, at ^ kTile);
       if (pos < it.wave_hi) w.template tile<2>(a, lk + at, lv + at, seen_of(it.row, pos, kKeys));
       if (more) {
-        St::template land<true>(t, kh, lk + (at ^ kTile));
-        St::template land<false>(t, vh, lv + (at ^ kTile));
+        st.template land<true>(kh, lk + (at ^ kTile));
+        st.template land<false>(vh, lv + (at ^ kTile));
       }
       wait_loads();
       meet();
@@ -783,12 +871,12 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
 // of the keys each, 32 at a time through LDS of their own: no wave waits for
 // another until their parts are joined at the end.
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool ONE>
 __global__ void __launch_bounds__(256, 1) k_attend_few(Args a) {
   constexpr int M = 32, kKeys = 32, kTile = kKeys * D * 2, kWaves = 4;
-  using St = Stage<D, E4M3, kKeys, 64>;
+  using St = Stage<D, E4M3, kKeys, 64, ONE>;
   __shared__ __align__(1024) uint8_t lds[kWaves][2][2][kTile];
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = threadIdx.x & 63;
+  const uint32_t wave = uniform(threadIdx.x >> 6), t = threadIdx.x & 63;
   uint32_t b = blockIdx.x;
   const uint32_t kv_head = b % a.heads;
   b /= a.heads;
@@ -804,35 +892,33 @@ __global__ void __launch_bounds__(256, 1) k_attend_few(Args a) {
   const uint32_t hi = it.range.hi;
   uint32_t pos = it.range.lo + wave * kKeys;
   uint8_t(*mine)[2][kTile] = lds[wave];
+  const St st(a, t);
   typename St::Held kh, vh;
   if (pos < hi) {
     const uint32_t add_blocks = kStep / a.bs, add_tokens = kStep % a.bs;
     typename St::Rows rows;
-    St::first(a, pos, t, rows);
-    St::look(it.range, rows);
-    typename St::Places at = St::place(a, rows, t, hi - pos);
-    St::template issue<true>(k, t, at, mine[0][0], kh);
-    St::template issue<false>(v, t, at, mine[0][1], vh);
-    St::template land<true>(t, kh, mine[0][0]);
-    St::template land<false>(t, vh, mine[0][1]);
-    St::next(a, add_blocks, add_tokens, rows);
-    St::look(it.range, rows);
+    const auto fetch = [&](uint32_t from, int x) {
+      const typename St::Places at = st.place(a, rows, hi - from);
+      st.template issue<true>(k, at, mine[x][0], kh);
+      st.template issue<false>(v, at, mine[x][1], vh);
+      st.next(a, add_blocks, add_tokens, rows);
+      st.look(it.range, rows);
+    };
+    st.first(a, pos, rows);
+    st.look(it.range, rows);
+    fetch(pos, 0);
+    st.template land<true>(kh, mine[0][0]);
+    st.template land<false>(vh, mine[0][1]);
     wait_loads();
     int x = 0;
 #pragma unroll 1
     for (; pos < hi; pos += kStep, x ^= 1) {  // hi + kStep fits 32 bits
       const bool more = pos + kStep < hi;
-      if (more) {
-        at = St::place(a, rows, t, hi - pos - kStep);
-        St::template issue<true>(k, t, at, mine[x ^ 1][0], kh);
-        St::template issue<false>(v, t, at, mine[x ^ 1][1], vh);
-        St::next(a, add_blocks, add_tokens, rows);
-        St::look(it.range, rows);
-      }
+      if (more) fetch(pos + kStep, x ^ 1);
       if (pos < it.wave_hi) w.template tile<1>(a, mine[x][0], mine[x][1], seen_of(it.row, pos, kKeys));
       if (more) {
-        St::template land<true>(t, kh, mine[x ^ 1][0]);
-        St::template land<false>(t, vh, mine[x ^ 1][1]);
+        st.template land<true>(kh, mine[x ^ 1][0]);
+        st.template land<false>(vh, mine[x ^ 1][1]);
       }
       wait_loads();
     }
@@ -952,23 +1038,30 @@ int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc
   return CLAIM_OK;
 }
 
-template <int D, bool E4M3>
-int launch(const PoolView& p, const Plan& plan, const Args& a) {
+template <int D, bool E4M3, bool ONE>
+int launch_one(const PoolView& p, const Plan& plan, const Args& a) {
   constexpr int kWaves = kRowsTile / 32;
   if (plan.few)
-    hipLaunchKernelGGL((k_attend_few<D, E4M3>), dim3(plan.tiles * a.heads * a.own_splits), dim3(256),
-                       0, p.stream, a);
+    hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE>), dim3(plan.tiles * a.heads * a.own_splits),
+                       dim3(256), 0, p.stream, a);
   else
-    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves>), dim3(plan.tiles * a.heads * a.own_splits),
-                       dim3(kWaves * 64), 0, p.stream, a, 0u);
+    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>),
+                       dim3(plan.tiles * a.heads * a.own_splits), dim3(kWaves * 64), 0, p.stream, a, 0u);
   if (plan.prefix_tiles)
-    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves>),
+    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>),
                        dim3(plan.prefix_tiles * a.heads * a.prefix_splits), dim3(kWaves * 64), 0,
                        p.stream, a, 1u);
   if (plan.parts)
     hipLaunchKernelGGL((k_join<D>), dim3((uint32_t)(((uint64_t)a.rows * a.heads * a.group + 3) / 4)),
                        dim3(256), 0, p.stream, a);
   return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;
+}
+
+template <int D, bool E4M3>
+int launch(const PoolView& p, const Plan& plan, const Args& a) {
+  // the rows of one load instruction in one block: see Stage
+  return p.bs % (64 * 16 / (D * (E4M3 ? 1 : 2))) == 0 ? launch_one<D, E4M3, true>(p, plan, a)
+                                                       : launch_one<D, E4M3, false>(p, plan, a);
 }
 
 }  // namespace
