@@ -66,7 +66,7 @@ struct Args {
   float2* part_ml;  // [row][query head][split]: maximum, sum
 };
 
-// One tile's query row of this lane.
+// A query row of this lane.
 struct Row {
   bool valid;
   uint32_t row, head;  // packed row, query head
@@ -108,22 +108,34 @@ constexpr uint64_t kZeros = ~0ull, kNaNs = ~1ull;
 
 // ------------------------------------------------------------ tiles in LDS
 //
-// A tile is 32 or 64 rows of D bf16 values, whole rows one after another, the
-// 16-byte chunks of a row exchanged by an exclusive or with bits of the row's
-// number, so that both ways of reading it touch every bank equally: K by 32
-// rows x one chunk, V by 8 rows x 64 bytes.
+// A tile is whole rows one after another, the 16-byte chunks of a row
+// exchanged by an exclusive or with bits of the row's number, so that every
+// way of reading it touches all banks equally.
 
+// Rows of D bf16 values read by 32 x 32 products: K by 32 rows x one chunk, V
+// by 8 rows x 64 bytes.
 template <int D>
-__device__ __forceinline__ uint32_t k_swizzle(uint32_t row) {
-  return D == 128 ? row & 15 : (row >> 1) & 7;
-}
+struct WideSwizzle {
+  static __device__ __forceinline__ constexpr uint32_t k(uint32_t row) {
+    return D == 128 ? row & 15 : (row >> 1) & 7;
+  }
+  static __device__ __forceinline__ constexpr uint32_t v(uint32_t row) {
+    return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+  }
+};
 
-template <int D>
-__device__ __forceinline__ uint32_t v_swizzle(uint32_t row) {
-  return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
-}
+// Rows of BYTES bytes, as they are in the pool, read by 16 x 16 products: 16
+// rows x 32 or 64 bytes.
+template <int BYTES>
+struct NarrowSwizzle {
+  static __device__ __forceinline__ constexpr uint32_t k(uint32_t row) {
+    return BYTES == 256 ? row & 15 : BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+  }
+  static __device__ __forceinline__ constexpr uint32_t v(uint32_t row) { return k(row); }
+};
 
 typedef const __attribute__((address_space(3))) u32x4 lds_words;
+typedef const __attribute__((address_space(3))) u32x2 lds_pair;
 
 __device__ __forceinline__ uint32_t lds_address(const uint8_t* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p;
@@ -161,25 +173,25 @@ __device__ __forceinline__ u32x4 widen(uint32_t a, uint32_t b) {
                two(b, std::true_type{})};
 }
 
-// Moves KEYS rows of one plane into a tile with THREADS threads.  bf16 rows go
-// straight to LDS; e4m3 rows are loaded into registers by issue() and widened
-// into LDS by land().
+// Moves KEYS rows of BYTES bytes of one plane into a tile with THREADS threads,
+// straight to LDS; or (WIDEN) e4m3 rows into registers by issue(), and widened
+// to bf16 into LDS by land().
 //
 // ONE: the rows that a wave loads with one instruction (4 of 256 bytes to 16
 // of 64) lie in one block, as they do wherever their number divides the block
 // size.  Block, token and address are then the wave's, on the scalar unit;
 // otherwise each lane has its own.  16384 causal tokens, 32 heads over 8 of
 // 128, blocks of 16: FIGURE-ONE.
-template <int D, bool E4M3, int KEYS, int THREADS, bool ONE>
+template <int BYTES, bool WIDEN, int KEYS, int THREADS, bool ONE, typename Swizzle>
 struct Stage {
-  static constexpr int kRowLanes = D * (E4M3 ? 1 : 2) / 16;  // lanes of one row
+  static constexpr int kRowLanes = BYTES / 16;  // lanes of one row
   static constexpr int kWaveRows = 64 / kRowLanes;
   static constexpr int kRows = THREADS / kRowLanes;  // rows of one step
   static constexpr int kSteps = KEYS / kRows ? KEYS / kRows : 1;
-  static_assert(E4M3 || KEYS % kRows == 0, "bf16 tiles are filled by whole steps");
+  static_assert(WIDEN || KEYS % kRows == 0, "tiles are filled by whole steps");
 
   struct Held {  // e4m3 bytes on their way
-    u32x4 r[E4M3 ? kSteps : 1];
+    u32x4 r[WIDEN ? kSteps : 1];
   };
 
   // The rows of one tile, a wave's first of each step (ONE) or a lane's own:
@@ -200,10 +212,8 @@ struct Stage {
   __device__ __forceinline__ Stage(const Args& a, uint32_t thread) : t(thread) {
     wave = THREADS == 64 ? 0 : uniform(thread >> 6);
     const uint32_t row = thread / kRowLanes, chunk = thread % kRowLanes;
-    // swizzles repeat every 16 rows: they are the same in every step
-    static_assert(kRows % 16 == 0 || kSteps == 1 || THREADS == 64, "");
-    k_off = (E4M3 ? chunk : chunk ^ k_swizzle<D>(row)) * 16;
-    v_off = (E4M3 ? chunk : chunk ^ v_swizzle<D>(row)) * 16;
+    k_off = (WIDEN ? chunk : chunk ^ Swizzle::k(row)) * 16;
+    v_off = (WIDEN ? chunk : chunk ^ Swizzle::v(row)) * 16;
     if (ONE) {
       k_off += row % kWaveRows * a.token_bytes;
       v_off += row % kWaveRows * a.token_bytes;
@@ -270,14 +280,14 @@ struct Stage {
     const uint32_t off = KEY ? k_off : v_off;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      if (E4M3 && KEYS < kRows && i * kRows + t / kRowLanes >= KEYS) break;
+      if (WIDEN && KEYS < kRows && i * kRows + t / kRowLanes >= KEYS) break;
       const uint32_t to = lds_address(tile) + i * THREADS * 16 + wave * 1024;
-      // swizzles of a step of 4 or 8 rows are its own
-      const uint32_t mine = THREADS == 64 && !E4M3 ? off ^ step_swizzle<KEY>(i) : off;
+      // the first row of a step has a swizzle of its own where a step is less than 16 rows
+      const uint32_t mine = WIDEN ? off : off ^ (KEY ? Swizzle::k(i * kRows) : Swizzle::v(i * kRows)) * 16;
       const uint8_t* base = ONE ? uniform(plane + p.byte[i]) : plane + p.byte[i];
       const bool fine = p.entry[i] != CLAIM_NONE && row(i) + (ONE ? kWaveRows : 1) <= p.left;
       if (ONE ? fine : __all(fine)) {
-        if constexpr (E4M3)
+        if constexpr (WIDEN)
           held.r[i] = *(const u32x4*)(base + mine);
         else if constexpr (ONE)
           copy_to_lds(base, mine, to);
@@ -288,7 +298,7 @@ struct Stage {
         const uint8_t* from = there && p.entry[i] != CLAIM_NONE
                                   ? base + mine
                                   : (const uint8_t*)kFill + (KEY && there ? 16 : 0);
-        if constexpr (E4M3)
+        if constexpr (WIDEN)
           held.r[i] = *(const u32x4*)from;
         else
           copy_to_lds(from, to);
@@ -296,23 +306,15 @@ struct Stage {
     }
   }
 
-  // What step i's swizzle adds to step 0's (a wave alone: a step is kWaveRows
-  // rows, and the swizzles repeat every 16).
-  template <bool KEY>
-  static __device__ __forceinline__ constexpr uint32_t step_swizzle(int i) {
-    return (KEY ? (D == 128 ? i * kWaveRows & 15 : (i * kWaveRows >> 1) & 7)
-                : (D == 128 ? (i * kWaveRows & 3) << 2 : ((i * kWaveRows >> 1) & 1) << 2)) * 16;
-  }
-
   template <bool KEY>
   __device__ __forceinline__ void land(const Held& held, uint8_t* tile) const {
-    if constexpr (E4M3) {
+    if constexpr (WIDEN) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         const uint32_t row = i * kRows + t / kRowLanes, chunk = 2 * (t % kRowLanes);
         if (KEYS < kRows && row >= KEYS) break;
-        const uint32_t x = KEY ? k_swizzle<D>(row) : v_swizzle<D>(row);
-        uint8_t* to = tile + row * D * 2;
+        const uint32_t x = KEY ? Swizzle::k(row) : Swizzle::v(row);
+        uint8_t* to = tile + row * BYTES * 2;
         *(u32x4*)(to + (chunk ^ x) * 16) = widen(held.r[i].x, held.r[i].y);
         *(u32x4*)(to + ((chunk + 1) ^ x) * 16) = widen(held.r[i].z, held.r[i].w);
       }
@@ -353,9 +355,9 @@ struct Wave {
     m = kNoMax;
     l = 0;
     const uint32_t lane = threadIdx.x & 63, row = lane & 31;
-    k_lane = row * D * 2 + ((h ^ k_swizzle<D>(row)) << 4);
+    k_lane = row * D * 2 + ((h ^ WideSwizzle<D>::k(row)) << 4);
     const uint32_t key = 4 * h + ((lane & 15) >> 2);
-    v_lane = key * D * 2 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D>(key)) << 4) +
+    v_lane = key * D * 2 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ WideSwizzle<D>::v(key)) << 4) +
              (lane & 1) * 8;
   }
 
@@ -576,97 +578,86 @@ struct Wave {
 
 // ------------------------------------------------------------- work items
 
-// The sequence whose tile `tile` (of M packed query rows) is.  Sequence s
-// starts at tile floor(first row x group / M) + s: an ascending bound that
-// leaves every sequence the tiles it needs.
-__device__ __forceinline__ uint64_t first_tile(const Args& a, uint32_t s, uint32_t M) {
-  const uint64_t first = a.offsets ? a.offsets[s] : s;
-  return first * a.group / M + s;
+// A tile of M packed query rows (token x query head of the group) that read
+// the same keys, and one split's share of those keys: all of it the wave's.
+struct Tile {
+  bool prefix, any;    // any: the tile has rows
+  uint32_t first, n;   // own: the sequence's first row and how many it has
+  uint32_t x0, all;    // the tile's first packed row, and how many there are
+  int64_t len;         // own: the sequence's tokens
+  uint32_t kv_head;
+  Range range;
+};
+
+// The last sequence whose tiles start at or before `tile`.  Sequence s starts
+// at tile floor(first row x group / M) + s: an ascending bound that leaves
+// every sequence the tiles it needs.
+template <int M>
+__device__ __forceinline__ uint32_t first_tile(const Args& a, uint32_t s) {
+  return a.offsets[s] * a.group / M + s;  // rows x group fits 32 bits
 }
 
-__device__ __forceinline__ uint32_t find_tile(const Args& a, uint32_t tile, uint32_t M) {
+template <int M>
+__device__ __forceinline__ uint32_t find_tile(const Args& a, uint32_t tile) {
   uint32_t lo = 0, hi = a.num_seqs;
   const uint32_t lane = threadIdx.x & 63;
   while (hi - lo > 1) {
     const uint32_t step = (hi - lo + 63) / 64, s = lo + lane * step;
-    const uint64_t m = __ballot(s < hi && first_tile(a, s, M) <= tile);
+    const uint64_t m = __ballot(s < hi && first_tile<M>(a, s) <= tile);
     lo += (m ? 63u - (uint32_t)__builtin_clzll(m) : 0u) * step;
     hi = lo + step < hi ? lo + step : hi;
   }
-  return lo;
+  return uniform(lo);
 }
 
-struct Item {
-  Row row;
-  Range range;
-  uint32_t wave_hi;  // positions at or past it are seen by no row of the wave
-  uint32_t all_below;  // every valid row of the wave sees the positions below it
-  uint32_t split;
-  bool any;          // the item has rows
-};
-
-// The rows of a tile of M, `r` this lane's among them, and the keys of one
-// split.
 template <int M>
-__device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t tile, uint32_t split,
-                                          uint32_t kv_head, uint32_t r, uint32_t align) {
-  Item it;
-  it.row.valid = false;
-  it.row.row = it.row.head = 0;
-  it.row.limit = 0;
-  it.any = false;
-  uint32_t splits;
-  int64_t top;  // limit of the tile's last row
+__device__ __forceinline__ Tile make_tile(const Args& a, bool prefix, uint32_t tile, uint32_t split,
+                                          uint32_t splits, uint32_t kv_head, uint32_t align) {
+  Tile it;
+  it.prefix = prefix;
+  it.kv_head = kv_head;
+  int64_t top;  // what the tile's last row sees
+  uint32_t lo = 0;
   if (prefix) {
-    const uint64_t x = (uint64_t)tile * M + r, all = (uint64_t)a.rows * a.group;
-    it.any = (uint64_t)tile * M < all;
-    if (x < all) {
-      const uint32_t row = (uint32_t)(x / a.group);
-      uint32_t s = row, n = 1, i = 0;
-      if (a.offsets) {
-        uint32_t lo = 0, hi = a.num_seqs;
-        while (hi - lo > 1) {
-          const uint32_t mid = (lo + hi) / 2;
-          if (a.offsets[mid] <= row) lo = mid; else hi = mid;
-        }
-        s = lo;
-        n = a.offsets[s + 1] - a.offsets[s];
-        i = row - a.offsets[s];
-      }
-      const uint32_t id = a.ids ? a.ids[s] : s;
-      it.row.valid = true;
-      it.row.row = row;
-      it.row.head = kv_head * a.group + (uint32_t)(x % a.group);
-      const int64_t limit = id < a.max_seqs ? (int64_t)a.lengths[id] - n + i + 1 : 0;
-      it.row.limit = (uint32_t)(limit < 0 ? 0 : limit < a.prefix_tokens ? limit : a.prefix_tokens);
-    }
-    it.range = Range{a.prefix, a.prefix_tokens / a.bs, 0, a.prefix_tokens};
-    splits = a.prefix_splits;
+    it.first = it.n = 0;
+    it.len = 0;
+    it.x0 = tile * M;
+    it.all = a.rows * a.group;
+    it.any = it.x0 < it.all;
+    it.range.list = a.prefix;
+    it.range.entries = a.prefix_tokens / a.bs;
     top = a.prefix_tokens;
-    it.split = a.own_splits + split;
   } else {
-    const uint32_t s = find_tile(a, tile, M);
-    const uint32_t first = a.offsets ? a.offsets[s] : s;
-    const uint32_t n = a.offsets ? a.offsets[s + 1] - first : 1;
-    const uint64_t x0 = ((uint64_t)tile - first_tile(a, s, M)) * M, x = x0 + r;
-    const uint64_t all = (uint64_t)n * a.group;
-    const uint32_t id = a.ids ? a.ids[s] : s;
-    // offsets that run backwards or past the rows give the sequence none
-    it.any = tile >= first_tile(a, s, M) && x0 < all && first <= a.rows && n <= a.rows - first;
-    const int64_t len = id < a.max_seqs ? a.lengths[id] : 0;
-    if (it.any && x < all) {
-      const uint32_t i = (uint32_t)(x / a.group);
-      it.row.valid = true;
-      it.row.row = first + i;
-      it.row.head = kv_head * a.group + (uint32_t)(x % a.group);
-      it.row.limit = len - n + i + 1 > 0 ? (uint32_t)(len - n + i + 1) : 0;
+    uint32_t s, part;
+    if (a.offsets) {
+      s = find_tile<M>(a, tile);
+      const uint32_t from = a.offsets[s], start = first_tile<M>(a, s);
+      it.first = from;
+      it.n = a.offsets[s + 1] - from;
+      part = tile - start;
+      // offsets that run backwards or past the rows give the sequence none
+      it.any = tile >= start && from <= a.rows && it.n <= a.rows - from;
+    } else {
+      const uint32_t per = (a.group + M - 1) / M;
+      s = per == 1 ? tile : tile / per;
+      part = tile - s * per;
+      it.first = s;
+      it.n = 1;
+      it.any = s < a.num_seqs;
+      if (!it.any) s = 0;
     }
-    const uint64_t last = x0 + M < all ? x0 + M : all;
-    top = it.any ? len - n + (int64_t)((last + a.group - 1) / a.group) : 0;
-    it.range = Range{a.tables + (uint64_t)(id < a.max_seqs ? id : 0) * a.max_blocks, a.max_blocks,
-                     a.prefix_tokens, 0};
-    splits = a.own_splits;
-    it.split = split;
+    it.all = it.any ? it.n * a.group : 0;
+    it.any = it.any && part <= it.all / M;
+    it.x0 = it.any ? part * M : 0;
+    it.any = it.any && it.x0 < it.all;
+    const uint32_t id = a.ids ? a.ids[s] : s;
+    const bool fine = id < a.max_seqs;
+    it.len = fine ? a.lengths[id] : 0;
+    it.range.list = a.tables + (uint64_t)(fine ? id : 0) * a.max_blocks;
+    it.range.entries = a.max_blocks;
+    lo = a.prefix_tokens;
+    const uint32_t last = it.x0 + M < it.all ? it.x0 + M : it.all;
+    top = it.any ? it.len - it.n + (last + a.group - 1) / a.group : 0;
   }
   // a row that sees a position past the table is NaN whatever else it sees:
   // one such position is enough, and a wrong length cannot hold the GPU
@@ -675,31 +666,64 @@ __device__ __forceinline__ Item make_item(const Args& a, bool prefix, uint32_t t
   end = end < 0xFFFFF000u ? end : 0xFFFFF000u;
   if (top > (int64_t)end + 1) top = (int64_t)end + 1;
   // this split's share of the keys from lo to the last row's limit
-  const uint32_t lo = it.range.lo;
-  const uint64_t keys = top > (int64_t)lo ? (uint64_t)top - lo : 0;
-  const uint64_t share = ((keys + splits - 1) / splits + align - 1) / align * align;
-  const uint64_t from = share * split < keys ? share * split : keys;
-  const uint64_t to = from + share < keys ? from + share : keys;
-  it.range.lo = uniform((uint32_t)(lo + from));
-  it.range.hi = uniform((uint32_t)(lo + to));
+  const uint32_t keys = top > (int64_t)lo ? (uint32_t)(top - lo) : 0;
+  uint32_t share = keys, from = 0;
+  if (splits > 1) {
+    share = (uint32_t)(((uint64_t)keys + splits - 1) / splits + align - 1) / align * align;
+    from = (uint64_t)share * split < keys ? share * split : keys;
+  }
+  const uint32_t to = keys - from < share ? keys : from + share;
+  it.range.lo = uniform(lo + from);
+  it.range.hi = uniform(lo + to);
   it.range.list = uniform(it.range.list);
   it.range.entries = uniform(it.range.entries);
-  // per wave: the most and the least that a row sees
-  uint32_t most = it.row.valid ? it.row.limit : 0, least = it.row.valid ? it.row.limit : ~0u;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint32_t x = __shfl_xor(most, d), y = __shfl_xor(least, d);
-    most = x > most ? x : most;
-    least = y < least ? y : least;
-  }
-  it.wave_hi = uniform(most);
-  it.all_below = uniform(least);
   return it;
 }
 
-// How many of the `keys` positions from `pos` on the row sees.
-__device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys) {
-  return r.limit <= pos ? 0 : r.limit - pos < keys ? (int)(r.limit - pos) : (int)keys;
+// Row r of the tile.
+__device__ __forceinline__ Row row_at(const Args& a, const Tile& it, uint32_t r) {
+  Row row;
+  const uint32_t x = it.x0 + r;
+  row.valid = it.any && x < it.all;
+  row.row = row.head = row.limit = 0;
+  if (!row.valid) return row;
+  uint32_t i = x / a.group, n = it.n;
+  row.head = it.kv_head * a.group + (x - i * a.group);
+  row.row = it.first + i;
+  int64_t len = it.len;
+  if (it.prefix) {
+    uint32_t s = row.row;
+    n = 1;
+    i = 0;
+    if (a.offsets) {
+      uint32_t lo = 0, hi = a.num_seqs;
+      while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.offsets[mid] <= row.row) lo = mid; else hi = mid;
+      }
+      s = lo;
+      n = a.offsets[s + 1] - a.offsets[s];
+      i = row.row - a.offsets[s];
+    }
+    const uint32_t id = a.ids ? a.ids[s] : s;
+    len = id < a.max_seqs ? a.lengths[id] : 0;
+  }
+  int64_t limit = len - n + i + 1;
+  if (it.prefix && limit > a.prefix_tokens) limit = a.prefix_tokens;
+  row.limit = limit > 0 ? (uint32_t)(limit < 0xFFFFFFFF ? limit : 0xFFFFFFFF) : 0;
+  return row;
+}
+
+// The most and the least that valid rows of `lanes` neighbouring lanes see.
+__device__ __forceinline__ void seen_by_wave(const Row& row, int lanes, uint32_t* most, uint32_t* least) {
+  uint32_t hi = row.valid ? row.limit : 0, lo = row.valid ? row.limit : ~0u;
+  for (int d = 1; d < lanes; d <<= 1) {
+    const uint32_t x = __shfl_xor(hi, d), y = __shfl_xor(lo, d);
+    hi = x > hi ? x : hi;
+    lo = y < lo ? y : lo;
+  }
+  *most = uniform(hi);
+  *least = uniform(lo);
 }
 
 // Everything that this wave has asked memory for has arrived.
@@ -708,13 +732,33 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// All but the last N copies to LDS have arrived.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N < 64, "");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0F70);
+  asm volatile("" ::: "memory");
+}
+
+// This wave's LDS reads and writes are done.
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);  // no work of one phase moves into the other
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads and writes are done
+  wait_lds();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
+}
+
+// How many of the `keys` positions from `pos` on the row sees.
+__device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys) {
+  return r.limit <= pos ? 0 : r.limit - pos < keys ? (int)(r.limit - pos) : (int)keys;
 }
 
 // ----------------------------------------------------------- many query rows
@@ -737,7 +781,7 @@ __device__ __forceinline__ void meet() {
 template <int D, bool E4M3, int WAVES, bool ONE>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
   constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2, kAhead = E4M3 ? 3 : 2;
-  using St = Stage<D, E4M3, kKeys, WAVES * 64, ONE>;
+  using St = Stage<D * (E4M3 ? 1 : 2), E4M3, kKeys, WAVES * 64, ONE, WideSwizzle<D>>;
   __shared__ __align__(1024) uint8_t lk[(kAhead + 1) * kTile];
   __shared__ __align__(1024) uint8_t lv[(kAhead + 1) * kTile];
   __shared__ uint32_t least[WAVES];
@@ -748,14 +792,16 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
   const uint32_t split = b % splits, tiles = prefix ? a.prefix_tiles : a.tiles;
   const uint32_t tile = tiles - 1 - b / splits;  // late rows see the most: they start first
-  const uint32_t r = (t >> 6) * 32 + (t & 31);
-  const Item it = make_item<M>(a, prefix, tile, split, kv_head, r, kKeys);
+  const Tile it = make_tile<M>(a, prefix, tile, split, splits, kv_head, kKeys);
   if (!it.any) return;
+  const Row row = row_at(a, it, (t >> 6) * 32 + (t & 31));
+  uint32_t wave_hi, wave_least;
+  seen_by_wave(row, 32, &wave_hi, &wave_least);
   const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
   const uint32_t lo = it.range.lo, hi = it.range.hi;
   // whole tiles that every row of the workgroup sees
-  if ((t & 63) == 0) least[t >> 6] = it.all_below;
+  if ((t & 63) == 0) least[t >> 6] = wave_least;
   __syncthreads();
   uint32_t below = hi;
 #pragma unroll
@@ -763,7 +809,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   const uint32_t full = uniform(below > lo ? (below - lo) / kKeys : 0);
 
   Wave<D> w;
-  w.start(a, it.row);
+  w.start(a, row);
   const St st(a, t);
   typename St::Held kh, vh;
   typename St::Rows rows;
@@ -853,7 +899,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
     for (; pos < hi; pos += kKeys, at ^= kTile) {  // hi + kKeys fits 32 bits
       const bool more = pos + kKeys < hi;
       if (more) fetch(pos + kKeys, at ^ kTile);
-      if (pos < it.wave_hi) w.template tile<2>(a, lk + at, lv + at, seen_of(it.row, pos, kKeys));
+      if (pos < wave_hi) w.template tile<2>(a, lk + at, lv + at, seen_of(row, pos, kKeys));
       if (more) {
         st.template land<true>(kh, lk + (at ^ kTile));
         st.template land<false>(vh, lv + (at ^ kTile));
@@ -862,156 +908,499 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
       meet();
     }
   }
-  w.finish(a, it.row, a.part_o != nullptr, it.split, a.own_splits + a.prefix_splits);
+  w.finish(a, row, a.part_o != nullptr, prefix ? a.own_splits + split : split,
+           a.own_splits + a.prefix_splits);
 }
 
 // ------------------------------------------------------------ few query rows
 //
-// Four waves of one workgroup hold the same (up to 32) rows and take a quarter
-// of the keys each, 32 at a time through LDS of their own: no wave waits for
-// another until their parts are joined at the end.
+// QT x 16 query rows of one sequence, as columns of 16 x 16 products, against a
+// long axis of keys.
+// Four waves hold the same rows and take every fourth group of KEYS keys
+// through LDS of their own, so no wave waits for another until their parts
+// are joined at the end.  K and V have two places each; the copy into one
+// begins as soon as what it held has been multiplied, so that one to two
+// groups are always on their way.  Bytes stay e4m3 in LDS and are widened on
+// the way into the product.
+//
+// A lane holds column lane % 16; of scores it has keys 4 (lane / 16) + r of
+// each 16, which is P^T's operand of a 16 x 16 x 16 product, and of a 16 x 16 x
+// 32 one over two groups of 16 if V^T's operand takes its keys in that order.
 
-template <int D, bool E4M3, bool ONE>
-__global__ void __launch_bounds__(256, 1) k_attend_few(Args a) {
-  constexpr int M = 32, kKeys = 32, kTile = kKeys * D * 2, kWaves = 4;
-  using St = Stage<D, E4M3, kKeys, 64, ONE>;
-  __shared__ __align__(1024) uint8_t lds[kWaves][2][2][kTile];
+template <int D, bool E4M3, int QT, int KEYS>
+struct Narrow {
+  static constexpr int kBytes = D * (E4M3 ? 1 : 2), kSub = KEYS / 16;
+  static_assert(KEYS == 32 || (KEYS == 16 && !E4M3), "");
+  bf16x8 q[QT][D / 32];
+  f32x4 o[QT][D / 16];
+  float m[QT], l[QT];  // the maximum is the row's; the sum this lane's share
+  uint32_t k_lane, v_lane;
+
+  __device__ __forceinline__ void start(const Args& a, const Row (&row)[QT]) {
+    const uint32_t lane = threadIdx.x & 63, g = lane >> 4, x = lane & 15;
+#pragma unroll
+    for (int c = 0; c < QT; ++c) {
+      const uint16_t* src = a.q + row[c].row * a.q_row + row[c].head * a.q_head + 8 * g;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) {
+        u32x4 w = {0, 0, 0, 0};
+        if (row[c].valid) w = *(const u32x4*)(src + 32 * t);
+        q[c][t] = __builtin_bit_cast(bf16x8, w);
+      }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{};
+      m[c] = kNoMax;
+      l[c] = 0;
+    }
+    using S = NarrowSwizzle<kBytes>;
+    if (E4M3) {
+      k_lane = x * kBytes + (((g >> 1) ^ S::k(x)) << 4) + (g & 1) * 8;
+      // rows of eight keys: 4 g .. 4 g + 3 and the same 16 on
+      const uint32_t r = x >> 1, key = 4 * g + (r & 3) + (r >> 2) * 16;
+      v_lane = key * kBytes + (S::v(key) << 4) + (x & 1) * 8;
+    } else {
+      k_lane = x * kBytes + ((g ^ S::k(x)) << 4);
+      const uint32_t key = 4 * g + (x >> 2);
+      v_lane = key * kBytes + ((((x & 3) >> 1) ^ S::v(key)) << 4) + (x & 1) * 8;
+    }
+  }
+
+  __device__ __forceinline__ void scores(const uint8_t* lk, f32x4 (&s)[QT][kSub]) const {
+    uint32_t at = lds_address(lk) + k_lane;
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int c = 0; c < QT; ++c)
+#pragma unroll
+      for (int n = 0; n < kSub; ++n) s[c][n] = f32x4{};
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int n = 0; n < kSub; ++n) {
+        const uint32_t x = (at ^ (t << (E4M3 ? 5 : 6))) + n * 16 * kBytes;
+        u32x4 w;
+        if (E4M3) {
+          const u32x2 e = *(const lds_pair*)(uintptr_t)x;
+          w = widen(e.x, e.y);
+        } else {
+          w = *(const lds_words*)(uintptr_t)x;
+        }
+#pragma unroll
+        for (int c = 0; c < QT; ++c)
+          s[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[c][t], s[c][n], 0, 0, 0);
+      }
+  }
+
+  // Weights of a group, and the running maximum and sum (see Wave::weights).
+  __device__ __forceinline__ void weights(const Args& a, f32x4 (&s)[QT][kSub], bool masked,
+                                          const int (&seen)[QT]) {
+    const int g4 = ((threadIdx.x >> 4) & 3) * 4;
+    float top[QT];
+    bool up = false;
+#pragma unroll
+    for (int c = 0; c < QT; ++c) {
+      float x = kNoMax;
+#pragma unroll
+      for (int n = 0; n < kSub; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (masked) s[c][n][r] = 16 * n + r < seen[c] - g4 ? s[c][n][r] : kNoMax;
+          x = fmaxf(x, s[c][n][r]);
+        }
+      const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      top[c] = across_halves_max(fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+      up |= top[c] > m[c] + a.margin || m[c] == kNoMax;
+    }
+    if (__any(up)) {
+#pragma unroll
+      for (int c = 0; c < QT; ++c) {
+        const float to = fmaxf(m[c], top[c]), base = to == kNoMax ? 0.0f : to;
+        const float f = __builtin_amdgcn_exp2f((m[c] - base) * a.c);
+        l[c] *= f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) o[c][j] *= f;
+        m[c] = to;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < QT; ++c) {
+      const float mc = m[c] == kNoMax ? 0.0f : m[c] * a.c;
+#pragma unroll
+      for (int n = 0; n < kSub; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[c][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], a.c, -mc));
+          l[c] += s[c][n][r];
+        }
+    }
+  }
+
+  // P^T's operand: keys 4 (lane / 16) + r of each group of 16
+  static __device__ __forceinline__ auto p_operand(const f32x4 (&s)[kSub]) {
+    if constexpr (KEYS == 16) {
+      s16x4 p;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[r] = __builtin_bit_cast(short, (__bf16)s[0][r]);
+      return p;
+    } else {
+      bf16x8 p;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = (__bf16)s[i / 4][i % 4];
+      return p;
+    }
+  }
+
+  // V^T's operand: 16 values of D from 16 j
+  static __device__ __forceinline__ auto v_operand(uint32_t at, int j) {
+    typedef __attribute__((address_space(3))) s16x4* p4;
+    if constexpr (E4M3) {
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      typedef __attribute__((address_space(3))) i32x2* p2;
+      const i32x2 e = __builtin_amdgcn_ds_read_tr8_b64_v2i32((p2)(uintptr_t)(at ^ (j << 4)));
+      return __builtin_bit_cast(bf16x8, widen((uint32_t)e.x, (uint32_t)e.y));
+    } else if constexpr (KEYS == 16) {
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)(at ^ (j << 5)));
+    } else {
+      const uint32_t x = at ^ (j << 5);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)x);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)(x + 16 * kBytes));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+
+  static __device__ __forceinline__ f32x4 multiply(s16x4 v, s16x4 p, f32x4 o) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, p, o, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 multiply(bf16x8 v, bf16x8 p, f32x4 o) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0);
+  }
+
+  __device__ __forceinline__ void values(const uint8_t* lv, const f32x4 (&s)[QT][kSub], bool masked,
+                                         const int (&seen)[QT]) {
+    uint32_t at = lds_address(lv) + v_lane;
+    asm volatile("" : "+v"(at));
+    if (masked && nonfinite(lv)) {
+      values_seen(at, s, seen);
+      return;
+    }
+    decltype(p_operand(s[0])) p[QT];
+#pragma unroll
+    for (int c = 0; c < QT; ++c) p[c] = p_operand(s[c]);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const auto v = v_operand(at, j);
+#pragma unroll
+      for (int c = 0; c < QT; ++c) o[c][j] = multiply(v, p[c], o[c][j]);
+    }
+  }
+
+  // Whether the tile of V holds an infinity or a NaN (e4m3 has only NaN).
+  __device__ __forceinline__ bool nonfinite(const uint8_t* lv) const {
+    bool bad = false;
+#pragma unroll 1
+    for (uint32_t at = (threadIdx.x & 63) * 16; at < KEYS * kBytes; at += 1024) {
+      const u32x4 w = *(const u32x4*)(lv + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (E4M3) {
+#pragma unroll
+          for (int y = 0; y < 32; y += 8) bad |= (w[i] >> y & 0x7Fu) == 0x7Fu;
+        } else {
+          bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+        }
+      }
+    }
+    return __any(bad);
+  }
+
+  // values() where V holds infinities or NaN that some rows do not see (see
+  // Wave::values_seen).
+  __device__ __forceinline__ void values_seen(uint32_t at, const f32x4 (&s)[QT][kSub], const int (&seen)[QT]) {
+    const int g4 = ((threadIdx.x >> 4) & 3) * 4;
+    constexpr int kN = KEYS == 16 ? 4 : 8;
+    constexpr uint16_t one = 0x3F80;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const auto v = v_operand(at, j);
+      typedef uint16_t u16xn __attribute__((ext_vector_type(kN)));
+      const u16xn w = __builtin_bit_cast(u16xn, v);
+      u16xn fine, high, low;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const bool bad = (w[i] & 0x7F80) == 0x7F80;
+        fine[i] = bad ? (uint16_t)0 : w[i];
+        high[i] = bad && w[i] != 0xFF80 ? one : (uint16_t)0;
+        low[i] = bad && w[i] != 0x7F80 ? one : (uint16_t)0;
+      }
+#pragma unroll
+      for (int c = 0; c < QT; ++c) {
+        u16xn sees;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) sees[i] = 16 * (i / 4) + i % 4 < seen[c] - g4 ? one : (uint16_t)0;
+        const auto p = p_operand(s[c]);
+        using V = decltype(v);
+        const V y = __builtin_bit_cast(V, sees);
+        o[c][j] = multiply(__builtin_bit_cast(V, fine), p, o[c][j]);
+        const f32x4 up = multiply(__builtin_bit_cast(V, high), y, f32x4{});
+        const f32x4 down = multiply(__builtin_bit_cast(V, low), y, f32x4{});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (up[r] > 0) o[c][j][r] += __builtin_inff();
+          if (down[r] > 0) o[c][j][r] -= __builtin_inff();
+        }
+      }
+    }
+  }
+};
+
+template <int D, bool E4M3, bool ONE, int QT>
+struct Few {
+  static constexpr int kWaves = 4, kBytes = D * (E4M3 ? 1 : 2);
+  static constexpr int kKeys = kBytes == 256 ? 16 : 32;  // LDS for two workgroups on a CU
+  static constexpr int kTile = kKeys * kBytes;
+  static constexpr int kLds = kWaves * 4 * kTile;
+};
+
+template <int D, bool E4M3, bool ONE, int QT>
+__global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
+  using F = Few<D, E4M3, ONE, QT>;
+  constexpr int M = 16 * QT, kKeys = F::kKeys, kTile = F::kTile, kWaves = F::kWaves;
+  using St = Stage<F::kBytes, false, kKeys, 64, ONE, NarrowSwizzle<F::kBytes>>;
+  __shared__ __align__(1024) uint8_t lds[F::kLds];
   const uint32_t wave = uniform(threadIdx.x >> 6), t = threadIdx.x & 63;
   uint32_t b = blockIdx.x;
   const uint32_t kv_head = b % a.heads;
   b /= a.heads;
   const uint32_t split = b % a.own_splits, tile = b / a.own_splits;
-  const Item it = make_item<M>(a, false, tile, split, kv_head, t & 31, kKeys);
+  const Tile it = make_tile<M>(a, false, tile, split, a.own_splits, kv_head, kKeys);
   if (!it.any) return;
-  const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
+  Row row[QT];
+  uint32_t least = ~0u;
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    row[c] = row_at(a, it, 16 * c + (t & 15));
+    uint32_t hi, lo;
+    seen_by_wave(row[c], 16, &hi, &lo);
+    least = lo < least ? lo : least;
+  }
+  const uint64_t head_bytes = (uint64_t)kv_head * F::kBytes;
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
-  Wave<D> w;
-  w.start(a, it.row);
-  // tiles wave, wave + 4, ... of the range
+  // groups wave, wave + 4, ... of the range
   constexpr uint32_t kStep = kWaves * kKeys;
   const uint32_t hi = it.range.hi;
   uint32_t pos = it.range.lo + wave * kKeys;
-  uint8_t(*mine)[2][kTile] = lds[wave];
+  uint8_t* const lk = lds + wave * 4 * kTile;
+  uint8_t* const lv = lk + 2 * kTile;
+  Narrow<D, E4M3, QT, kKeys> w;
   const St st(a, t);
-  typename St::Held kh, vh;
   if (pos < hi) {
     const uint32_t add_blocks = kStep / a.bs, add_tokens = kStep % a.bs;
-    typename St::Rows rows;
-    const auto fetch = [&](uint32_t from, int x) {
-      const typename St::Places at = st.place(a, rows, hi - from);
-      st.template issue<true>(k, at, mine[x][0], kh);
-      st.template issue<false>(v, at, mine[x][1], vh);
+    typename St::Rows rows, second;
+    typename St::Held none;
+    st.first(a, pos, rows);
+    second = rows;
+    st.next(a, add_blocks, add_tokens, second);
+    st.look(it.range, rows);
+    st.look(it.range, second);
+    typename St::Places at = st.place(a, rows, hi - pos);
+    st.template issue<true>(k, at, lk, none);
+    st.template issue<false>(v, at, lv, none);
+    const auto rest = [&](uint32_t from) { return from < hi ? hi - from : 0; };
+    at = st.place(a, second, rest(pos + kStep));
+    st.template issue<true>(k, at, lk + kTile, none);
+    st.template issue<false>(v, at, lv + kTile, none);
+    rows = second;
+    st.next(a, add_blocks, add_tokens, rows);
+    st.look(it.range, rows);
+    w.start(a, row);
+    uint32_t x = 0;
+    constexpr int kLater = 3 * St::kSteps;  // copies begun after the one that is waited for
+    const auto group = [&](auto masked) {
+      f32x4 s[QT][kKeys / 16];
+      int seen[QT];
+#pragma unroll
+      for (int c = 0; c < QT; ++c) seen[c] = masked ? seen_of(row[c], pos, kKeys) : kKeys;
+      at = st.place(a, rows, rest(pos + 2 * kStep));
       st.next(a, add_blocks, add_tokens, rows);
       st.look(it.range, rows);
+      wait_copies<kLater>();
+      w.scores(lk + x, s);
+      wait_lds();
+      st.template issue<true>(k, at, lk + x, none);
+      w.weights(a, s, masked, seen);
+      wait_copies<kLater>();
+      w.values(lv + x, s, masked, seen);
+      wait_lds();
+      st.template issue<false>(v, at, lv + x, none);
     };
-    st.first(a, pos, rows);
-    st.look(it.range, rows);
-    fetch(pos, 0);
-    st.template land<true>(kh, mine[0][0]);
-    st.template land<false>(vh, mine[0][1]);
-    wait_loads();
-    int x = 0;
+    // groups that all rows see, then the others; hi + 2 kStep fits 32 bits
+    const uint32_t whole = least < hi ? least : hi;
 #pragma unroll 1
-    for (; pos < hi; pos += kStep, x ^= 1) {  // hi + kStep fits 32 bits
-      const bool more = pos + kStep < hi;
-      if (more) fetch(pos + kStep, x ^ 1);
-      if (pos < it.wave_hi) w.template tile<1>(a, mine[x][0], mine[x][1], seen_of(it.row, pos, kKeys));
-      if (more) {
-        st.template land<true>(kh, mine[x ^ 1][0]);
-        st.template land<false>(vh, mine[x ^ 1][1]);
+    for (; pos + kKeys <= whole; pos += kStep, x ^= kTile) group(std::false_type{});
+#pragma unroll 1
+    for (; pos < hi; pos += kStep, x ^= kTile) group(std::true_type{});
+    wait_loads();
+  } else {
+    w.start(a, row);
+  }
+  // join the waves: each row's common maximum first, then two and two
+  __shared__ float tops[kWaves][M], sums[kWaves][M];
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    if (t < 16) tops[wave][16 * c + t] = w.m[c];
+    w.l[c] += __shfl_xor(w.l[c], 16);
+    w.l[c] += __shfl_xor(w.l[c], 32);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    float m = kNoMax;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) m = fmaxf(m, tops[i][16 * c + (t & 15)]);
+    const float f = w.m[c] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f((w.m[c] - m) * a.c);
+    w.m[c] = m;
+    if (t < 16) sums[wave][16 * c + t] = w.l[c] * f;  // a wave that saw nothing adds zeros
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) w.o[c][j] *= f;
+  }
+  constexpr uint32_t kPart = M * D;  // floats of one wave
+  static_assert(kPart * 4 * 2 <= F::kLds, "two waves' parts fit");
+  float* const parts = (float*)lds;
+#pragma unroll
+  for (uint32_t half = kWaves / 2; half > 0; half /= 2) {
+    float* mine = parts + (wave % half) * kPart;
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int c = 0; c < QT; ++c)
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) *(f32x4*)(mine + ((c * (D / 16) + j) * 64 + t) * 4) = w.o[c][j];
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int c = 0; c < QT; ++c)
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) w.o[c][j] += *(const f32x4*)(mine + ((c * (D / 16) + j) * 64 + t) * 4);
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  const uint32_t all = a.own_splits + a.prefix_splits, g4 = (t >> 4) * 4;
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    if (!row[c].valid) continue;
+    w.l[c] = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) w.l[c] += sums[i][16 * c + (t & 15)];
+    if (a.part_o) {
+      const uint64_t to = ((uint64_t)row[c].row * a.heads * a.group + row[c].head) * all + split;
+      if (t < 16) a.part_ml[to] = float2{w.m[c], w.l[c]};
+      if (w.l[c] == 0.0f) continue;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) *(f32x4*)(a.part_o + to * D + 16 * j + g4) = w.o[c][j];
+    } else {
+      const float f = w.l[c] == 0.0f ? 0.0f : a.v_scale / w.l[c];
+      uint16_t* dst = a.out + row[c].row * a.out_row + row[c].head * a.out_head + g4;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 e;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = (__bf16)(w.o[c][j][r] * f);
+        *(bf16x4*)(dst + 16 * j) = e;
       }
-      wait_loads();
     }
   }
-  // join the four waves: each row's common maximum first
-  __shared__ float top[kWaves][32];
-  if (t < 32) top[wave][t] = w.m;
-  __syncthreads();
-  float m = kNoMax;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) m = fmaxf(m, top[i][t & 31]);
-  const float f = w.m == kNoMax ? 0.0f : __builtin_amdgcn_exp2f((w.m - m) * a.c);
-  // a wave that saw nothing adds zeros
-  float* sums = (float*)&lds[0][0][0][0];  // [wave][D / 32 + 1][16][64]
-  float* part = sums + wave * (D / 32 * 16 + 1) * 64;
-#pragma unroll
-  for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) part[(j * 16 + r) * 64 + t] = w.o[j][r] * f;
-  part[D / 32 * 16 * 64 + t] = w.l * f;
-  __syncthreads();
-  if (wave != 0) return;
-  w.m = m;
-#pragma unroll
-  for (int i = 1; i < kWaves; ++i) {
-    const float* p = sums + i * (D / 32 * 16 + 1) * 64;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) w.o[j][r] = (i == 1 ? w.o[j][r] * f : w.o[j][r]) + p[(j * 16 + r) * 64 + t];
-    w.l = (i == 1 ? w.l * f : w.l) + p[D / 32 * 16 * 64 + t];
-  }
-  w.finish(a, it.row, a.part_o != nullptr, it.split, a.own_splits + a.prefix_splits);
 }
 
 // ------------------------------------------------------------------ joining
 
-// A wave joins the parts of one row and query head: D / 64 values a lane.
+constexpr uint32_t kMostSplits = 64;  // of either kind: two parts to a lane of the joining wave
+
+// A wave joins the parts of one row and query head: 16 bytes a lane, 64 / (D /
+// 4) parts at a time, four such loads in flight.
 template <int D>
 __global__ void __launch_bounds__(256) k_join(Args a) {
+  constexpr uint32_t kLanes = D / 4, kSide = 64 / kLanes;
   const uint32_t heads = a.heads * a.group, splits = a.own_splits + a.prefix_splits;
-  const uint64_t x = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t x = blockIdx.x * 4 + uniform(threadIdx.x >> 6);
   const uint32_t lane = threadIdx.x & 63;
-  if (x >= (uint64_t)a.rows * heads) return;
-  const float2* ml = a.part_ml + x * splits;
-  float m = kNoMax;
-  for (uint32_t s = lane; s < splits; s += 64) m = fmaxf(m, ml[s].x);
+  if (x >= a.rows * heads) return;
+  const float2* ml = a.part_ml + (uint64_t)x * splits;
+  float2 p[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) p[i] = lane + 64 * i < splits ? ml[lane + 64 * i] : float2{kNoMax, 0.0f};
+  float m = fmaxf(p[0].x, p[1].x);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  float o[D / 64] = {}, l = 0;
-  for (uint32_t s = 0; s < splits; ++s) {
-    const float2 p = ml[s];
-    if (p.y == 0.0f) continue;  // this part saw nothing (a NaN sum is not 0)
-    const float f = __builtin_amdgcn_exp2f((p.x - m) * a.c);
-    l += p.y * f;
-    const float* src = a.part_o + (x * splits + s) * D + lane * (D / 64);
+  float f[2], l = 0;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) o[i] += src[i] * f;
+  for (int i = 0; i < 2; ++i) {
+    // a part that saw nothing has sum 0 (a NaN sum is not 0)
+    f[i] = p[i].y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((p[i].x - m) * a.c);
+    l += p[i].y * f[i];
+    if (p[i].y == 0.0f) f[i] = -1.0f;  // nothing to read
   }
-  const float f = l == 0.0f ? 0.0f : a.v_scale / l;
-  uint16_t* dst = a.out + x / heads * a.out_row + x % heads * a.out_head + lane * (D / 64);
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) ((__bf16*)dst)[i] = (__bf16)(o[i] * f);
+  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+  const float* src = a.part_o + (uint64_t)x * splits * D + lane % kLanes * 4;
+  f32x4 o = {};
+  for (uint32_t s0 = 0; s0 < splits; s0 += 4 * kSide) {
+    f32x4 v[4];
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t s = s0 + i * kSide + lane / kLanes;
+      const float w0 = __shfl(f[0], s & 63), w1 = __shfl(f[1], s & 63);
+      w[i] = s >= splits ? -1.0f : s < 64 ? w0 : w1;
+      v[i] = f32x4{};
+      if (!(w[i] < 0)) v[i] = *(const f32x4*)(src + (uint64_t)s * D);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!(w[i] < 0)) o += v[i] * w[i];
+  }
+#pragma unroll
+  for (uint32_t d = kLanes; d < 64; d <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
+  if (lane >= kLanes) return;
+  const float y = l == 0.0f ? 0.0f : a.v_scale / l;
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  bf16x4 e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e[i] = (__bf16)(o[i] * y);
+  *(bf16x4*)(a.out + x / heads * a.out_row + x % heads * a.out_head + lane * 4) = e;
 }
 
 // --------------------------------------------------------------------- host
 
 struct Plan {
-  bool few;  // own keys by k_attend_few
+  uint32_t columns;  // own keys by k_attend_few with 16 x columns rows a tile; 0: by k_attend_rows
   uint32_t own_splits, prefix_splits, tiles, prefix_tiles;
   uint64_t parts;  // parts of all rows and heads; 0: none are kept
 };
 
-constexpr uint32_t kRowsTile = 256;
-
-uint32_t splits_for(uint64_t groups, uint64_t want, uint64_t keys, uint64_t least) {
-  // enough workgroups for the GPU, no share shorter than `least` keys
-  const uint64_t s = groups ? (want + groups - 1) / groups : 1;
-  const uint64_t most = keys / least;
+constexpr uint32_t kRowsTile = 256;  // rows of k_attend_rows' tile
+// Splits of `keys` for `groups` workgroups where `slots` run at a time: all of
+// them in one round, no share shorter than `least` keys.
+uint32_t splits_for(uint64_t groups, uint64_t slots, uint64_t keys, uint64_t least) {
+  const uint64_t s = groups ? slots / groups : 1, most = keys / least;
   const uint64_t got = s < most ? s : most;
-  return (uint32_t)(got < 1 ? 1 : got > 256 ? 256 : got);
+  return (uint32_t)(got < 1 ? 1 : got > kMostSplits ? kMostSplits : got);
 }
 
 Plan make_plan(const PoolView& p, const claim_seqs* s, const claim_attend_desc* d) {
   Plan r{};
-  const uint64_t group = d->num_heads / p.heads, rows = d->kv.num_rows;
+  const uint64_t group = d->num_heads / p.heads, rows = d->kv.num_rows, seqs = d->kv.num_seqs;
   const uint64_t prefix = (uint64_t)d->prefix_blocks * p.bs;
   const uint64_t table = (uint64_t)s->max_blocks * p.bs;
   const uint64_t own = table > prefix ? table - prefix : 0;
-  r.few = rows * group <= 32ull * d->kv.num_seqs;
-  const uint32_t M = r.few ? 32 : kRowsTile;
-  r.tiles = (uint32_t)(rows * group / M + d->kv.num_seqs);
-  r.own_splits = splits_for((uint64_t)r.tiles * p.heads, r.few ? 2 * p.cus : p.cus, own, r.few ? 256 : 512);
+  const uint64_t each = (rows * group + seqs - 1) / seqs;  // query rows of a sequence
+  r.columns = each <= 16 ? 1 : each <= 64 ? 2 : 0;
+  const uint32_t M = r.columns ? 16 * r.columns : kRowsTile;
+  r.tiles = (uint32_t)(d->kv.offsets ? rows * group / M + seqs : seqs * ((group + M - 1) / M));
+  r.own_splits = splits_for((uint64_t)r.tiles * p.heads, r.columns ? 2ull * p.cus : p.cus, own,
+                            r.columns ? 256 : 512);
   if (prefix) {
     r.prefix_tiles = (uint32_t)((rows * group + kRowsTile - 1) / kRowsTile);
     r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, p.cus, prefix, 256);
@@ -1041,19 +1430,19 @@ int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc
 template <int D, bool E4M3, bool ONE>
 int launch_one(const PoolView& p, const Plan& plan, const Args& a) {
   constexpr int kWaves = kRowsTile / 32;
-  if (plan.few)
-    hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE>), dim3(plan.tiles * a.heads * a.own_splits),
-                       dim3(256), 0, p.stream, a);
-  else
-    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>),
-                       dim3(plan.tiles * a.heads * a.own_splits), dim3(kWaves * 64), 0, p.stream, a, 0u);
+  const dim3 own(plan.tiles * a.heads * a.own_splits);
+  switch (plan.columns) {
+    case 1: hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 1>), own, dim3(256), 0, p.stream, a); break;
+    case 2: hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 2>), own, dim3(256), 0, p.stream, a); break;
+    default:
+      hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>), own, dim3(kWaves * 64), 0, p.stream, a, 0u);
+  }
   if (plan.prefix_tiles)
     hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>),
                        dim3(plan.prefix_tiles * a.heads * a.prefix_splits), dim3(kWaves * 64), 0,
                        p.stream, a, 1u);
   if (plan.parts)
-    hipLaunchKernelGGL((k_join<D>), dim3((uint32_t)(((uint64_t)a.rows * a.heads * a.group + 3) / 4)),
-                       dim3(256), 0, p.stream, a);
+    hipLaunchKernelGGL((k_join<D>), dim3((a.rows * a.heads * a.group + 3) / 4), dim3(256), 0, p.stream, a);
   return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;
 }
 
