@@ -272,6 +272,7 @@ class Pool:
             stream = torch.cuda.current_stream(kv.device)
         self.kv = kv
         self.stream = stream
+        self._stream_at = stream.cuda_stream
         self.geometry = geometry
         self.seed = seed
         d = PoolDesc(
@@ -480,7 +481,9 @@ class Pool:
         """A with-block whose pool calls come after what the current stream
         has queued, and before what it queues next, also where the pool's
         stream is another one; ``tensors`` are the arguments of those calls."""
-        return _Ordered(self.stream, tensors)
+        if _torch().cuda.current_stream(self.kv.device).cuda_stream == self._stream_at:
+            return _SAME_STREAM
+        return _OtherStream(self.stream, tensors)
 
     def timing(self) -> dict:
         t = CTiming()
@@ -488,15 +491,23 @@ class Pool:
         return {name: getattr(t, name) for name, _ in CTiming._fields_}
 
 
-class _Ordered:
-    __slots__ = ("stream", "current")
+class _SameStream:
+    """Work queued on one stream is in order already."""
 
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        pass
+
+
+_SAME_STREAM = _SameStream()
+
+
+class _OtherStream:
     def __init__(self, stream, tensors):
         self.stream = stream
         self.current = _torch().cuda.current_stream(stream.device)
-        if self.current.cuda_stream == stream.cuda_stream:
-            self.current = None
-            return
         stream.wait_stream(self.current)
         for t in tensors:
             if t is not None:
@@ -506,8 +517,7 @@ class _Ordered:
         return self
 
     def __exit__(self, *exc):
-        if self.current is not None:
-            self.current.wait_stream(self.stream)
+        self.current.wait_stream(self.stream)
 
 
 def _device_ints(device, **tensors) -> None:

@@ -445,34 +445,24 @@ struct Wave {
   }
 
   // values() of one tile of 64 keys, then scores() of another: operands are
-  // read from LDS two groups of four products ahead of their use.
+  // read from LDS four products ahead of their use.
   __device__ __forceinline__ void multiply(const uint8_t* lv, const bf16x8 (&p)[2][2], const uint8_t* lk,
                                            f32x16 (&s)[2]) {
     values<2>(lv, p);
     scores<2>(lk, s);
-    constexpr int kV = D / 32, kK = D / 32;  // products of a group; groups of K operands
-    constexpr int kRead = 0x100, kMul = 0x8;
-    __builtin_amdgcn_sched_group_barrier(kRead, 4 * kV, 0);
+    constexpr int kV = D / 32, kAll = D / 8, kRead = 0x100, kMul = 0x8;  // products of a step of V; of K
+    __builtin_amdgcn_sched_group_barrier(kRead, 8, 0);
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int i = 0; i < 4 * kV - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+    }
 #pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
-      }
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kRead, 4 / kV, 0);
-      }
-#pragma unroll
-    for (int g = 0; g < 4 * (kK - 2); ++g) {
+    for (int i = 0; i < kAll; ++i) {
       __builtin_amdgcn_sched_group_barrier(kMul, 1, 0);
       __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kMul, 8, 0);
+    __builtin_amdgcn_sched_group_barrier(kMul, 4, 0);
   }
 
   // A whole tile of which the lane's row sees the first `seen` keys.
@@ -505,39 +495,29 @@ struct Wave {
     return __any(bad);
   }
 
-  // values() where V holds infinities or NaN that some rows do not see: the
-  // product over finite values, then for each place whether a row sees an
-  // infinity of either sign or a NaN there (products of ones and zeros).
+  // values() where V holds infinities or NaN that some rows do not see: one
+  // key's product at a time, kept by the rows that see the key.
   template <int U>
   __device__ __forceinline__ void values_seen(const uint8_t* lv, const bf16x8 (&p)[U][2], int seen) {
-    const int h = (threadIdx.x >> 5) & 1;
-    const uint32_t at = lds_address(lv) + v_lane;
-    const __bf16 zero = (__bf16)0.0f, one = (__bf16)1.0f;
+    const uint32_t at = lds_address(lv) + v_lane, h = (threadIdx.x >> 5) & 1;
+#pragma unroll 1
+    for (uint32_t key = 0; key < 32 * U; ++key) {
+      // the key's element of an operand: half (key / 4) % 2, place (key / 8) % 2 * 4 + key % 4
+      const uint32_t place = (key >> 3 & 1) * 4 + (key & 3);
+      const uint32_t half = (key >> 2 & 1) == h ? 0xFFFFu << (place & 1) * 16 : 0;
+      u32x4 only, w = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      f32x16 up = {}, down = {};  // infinities seen; a NaN counts as both
+      for (int i = 0; i < 4; ++i) only[i] = place / 2 == (uint32_t)i ? half : 0;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int x = 0; x < 2 * U; ++x)
+        if (key / 16 == (uint32_t)x) w = __builtin_bit_cast(u32x4, p[x / 2][x % 2]);
+      const bf16x8 weight = __builtin_bit_cast(bf16x8, w & only);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const bf16x8 v = v_operand(at, u, t, j);
-          bf16x8 fine, high, low, sees;
+      for (int j = 0; j < D / 32; ++j) {
+        const u32x4 v = __builtin_bit_cast(u32x4, v_operand(at + key / 16 * 16 * D * 2, 0, 0, j)) & only;
+        const f32x16 with = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), weight, o[j], 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint16_t w = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
-            fine[i] = (w & 0x7F80) == 0x7F80 ? zero : v[i];
-            high[i] = (w & 0x7F80) == 0x7F80 && w != 0xFF80 ? one : zero;
-            low[i] = (w & 0x7F80) == 0x7F80 && w != 0x7F80 ? one : zero;
-            sees[i] = 32 * u + 16 * t + 8 * (i / 4) + i % 4 < seen - 4 * h ? one : zero;
-          }
-          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fine, p[u][t], o[j], 0, 0, 0);
-          up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(high, sees, up, 0, 0, 0);
-          down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(low, sees, down, 0, 0, 0);
-        }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (up[r] > 0) o[j][r] += __builtin_inff();
-        if (down[r] > 0) o[j][r] -= __builtin_inff();
+        for (int r = 0; r < 16; ++r) o[j][r] = (int)key < seen ? with[r] : o[j][r];
       }
     }
   }
@@ -794,80 +774,94 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   const uint32_t tile = tiles - 1 - b / splits;  // late rows see the most: they start first
   const Tile it = make_tile<M>(a, prefix, tile, split, splits, kv_head, kKeys);
   if (!it.any) return;
-  const Row row = row_at(a, it, (t >> 6) * 32 + (t & 31));
-  uint32_t wave_hi, wave_least;
-  seen_by_wave(row, 32, &wave_hi, &wave_least);
   const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
   const uint32_t lo = it.range.lo, hi = it.range.hi;
-  // whole tiles that every row of the workgroup sees
-  if ((t & 63) == 0) least[t >> 6] = wave_least;
-  __syncthreads();
-  uint32_t below = hi;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) below = least[w] < below ? least[w] : below;
-  const uint32_t full = uniform(below > lo ? (below - lo) / kKeys : 0);
-
-  Wave<D> w;
-  w.start(a, row);
   const St st(a, t);
   typename St::Held kh, vh;
   typename St::Rows rows;
-  if (full) {
-    const uint32_t add_blocks = kKeys / a.bs, add_tokens = kKeys % a.bs;
-    typename St::Places kp, vp;
-    // tiles 0 and 1 of K and 0 of V, then what W(-1) would have asked for;
-    // tiles past the full ones are copied too, and nothing reads them
+  typename St::Places kp, vp;
+  const uint32_t add_blocks = kKeys / a.bs, add_tokens = kKeys % a.bs;
+  const auto left = [&](uint32_t tile) {  // rows of the tile that the range has
+    const uint32_t from = lo + tile * kKeys;
+    return from < hi ? hi - from : 0;
+  };
+  // copies begin before anything else: tiles 0 and 1 of K and 0 of V, then
+  // what W(-1) would have asked for
+  {
+    typename St::Rows ahead[kAhead];
+    typename St::Held first[2];
     st.first(a, lo, rows);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      ahead[i] = rows;
+      st.look(it.range, ahead[i]);
+      st.next(a, add_blocks, add_tokens, rows);
+    }
     st.look(it.range, rows);
-    vp = st.place(a, rows, kKeys);
-    st.template issue<true>(k, vp, lk, kh);
+    vp = st.place(a, ahead[0], left(0));
+    kp = st.place(a, ahead[1], left(1));
+    st.template issue<true>(k, vp, lk, first[0]);
     st.template issue<false>(v, vp, lv, vh);
-    st.template land<true>(kh, lk);
+    st.template issue<true>(k, kp, lk + kTile, first[1]);
+    st.template land<true>(first[0], lk);
     st.template land<false>(vh, lv);
-    st.next(a, add_blocks, add_tokens, rows);
-    st.look(it.range, rows);
-    kp = st.place(a, rows, kKeys);
-    st.template issue<true>(k, kp, lk + kTile, kh);
-    st.template land<true>(kh, lk + kTile);
-    st.next(a, add_blocks, add_tokens, rows);
-    st.look(it.range, rows);
+    st.template land<true>(first[1], lk + kTile);
     if (E4M3) {
       vp = kp;
-      kp = st.place(a, rows, kKeys);
+      kp = st.place(a, ahead[kAhead - 1], left(2));
       st.template issue<true>(k, kp, lk, kh);
       st.template issue<false>(v, vp, lv, vh);
-      st.next(a, add_blocks, add_tokens, rows);
-      st.look(it.range, rows);
     }
-    wait_loads();
-    meet();
+  }
+  const Row row = row_at(a, it, (t >> 6) * 32 + (t & 31));
+  Wave<D> w;
+  w.start(a, row);
+  uint32_t wave_hi, wave_least;
+  seen_by_wave(row, 32, &wave_hi, &wave_least);
+  // whole tiles that every row of the workgroup sees
+  if ((t & 63) == 0) least[t >> 6] = wave_least;
+  wait_loads();
+  meet();
+  uint32_t below = hi;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) below = least[i] < below ? least[i] : below;
+  const uint32_t full = uniform(below > lo ? (below - lo) / kKeys : 0);
+
+  uint32_t now = 0, n = 0;  // tile n is at `now` in the ring
+  const auto before = [&](uint32_t x) { return x ? x - kTile : kAhead * kTile; };
+  const auto fetch = [&] {
+    const uint32_t to = before(now);  // tile n + A of K takes the place of n - 1
+    if (E4M3) {  // what W(n - 1) asked for: tile n + A - 1 of K, n + A - 2 of V
+      st.template land<true>(kh, lk + before(to));
+      st.template land<false>(vh, lv + before(before(to)));
+    }
+    vp = kp;
+    kp = st.place(a, rows, left(n + kAhead));
+    st.template issue<true>(k, kp, lk + to, kh);
+    st.template issue<false>(v, vp, lv + before(to), vh);
+    st.next(a, add_blocks, add_tokens, rows);
+    st.look(it.range, rows);
+  };
+  const auto step = [&] {
+    now = now == kAhead * kTile ? 0 : now + kTile;
+    ++n;
+  };
+  if (full) {
     if (uniform(t >> 6) >= WAVES / 2) meet();  // these waves are a phase behind
     f32x16 s[2];
     bf16x8 p[2][2];
-    uint32_t now = 0;                                  // where tile n is in the ring
-    const auto before = [&](uint32_t x) { return x ? x - kTile : kAhead * kTile; };
     const auto weigh = [&] {
-      const uint32_t to = before(now);  // tile n + A of K takes the place of n - 1
-      if (E4M3) {  // what W(n - 1) asked for: tile n + A - 1 of K, n + A - 2 of V
-        st.template land<true>(kh, lk + before(to));
-        st.template land<false>(vh, lv + before(before(to)));
-      }
-      vp = kp;
-      kp = st.place(a, rows, kKeys);
-      st.template issue<true>(k, kp, lk + to, kh);
-      st.template issue<false>(v, vp, lv + before(to), vh);
-      st.next(a, add_blocks, add_tokens, rows);
-      st.look(it.range, rows);
+      fetch();
       w.template weights<2>(a, s, p);
-      now = now == kAhead * kTile ? 0 : now + kTile;
+      step();
       meet();
     };
     w.template scores<2>(lk, s);
     meet();
     weigh();
 #pragma unroll 1
-    for (uint32_t n = 1; n < full; ++n) {
+    while (n < full) {
       __builtin_amdgcn_s_setprio(1);
       w.multiply(lv + before(now), p, lk + now, s);
       __builtin_amdgcn_s_setprio(0);
@@ -880,33 +874,15 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
     if (uniform(t >> 6) < WAVES / 2) meet();
     meet();
   }
-  uint32_t pos = lo + full * kKeys;
-  if (pos < hi) {
-    const auto fetch = [&](uint32_t from, uint32_t buffer) {
-      st.first(a, from, rows);
-      st.look(it.range, rows);
-      const typename St::Places at = st.place(a, rows, hi - from);
-      st.template issue<true>(k, at, lk + buffer, kh);
-      st.template issue<false>(v, at, lv + buffer, vh);
-    };
-    fetch(pos, 0);
-    st.template land<true>(kh, lk);
-    st.template land<false>(vh, lv);
+#pragma unroll 1
+  for (uint32_t pos = lo + full * kKeys; pos < hi; pos += kKeys) {  // hi + kKeys fits 32 bits
+    const bool more = pos + kKeys < hi;
+    if (more) fetch();
+    if (pos < wave_hi) w.template tile<2>(a, lk + now, lv + now, seen_of(row, pos, kKeys));
+    if (!more) break;
+    step();
     wait_loads();
     meet();
-    uint32_t at = 0;
-#pragma unroll 1
-    for (; pos < hi; pos += kKeys, at ^= kTile) {  // hi + kKeys fits 32 bits
-      const bool more = pos + kKeys < hi;
-      if (more) fetch(pos + kKeys, at ^ kTile);
-      if (pos < wave_hi) w.template tile<2>(a, lk + at, lv + at, seen_of(row, pos, kKeys));
-      if (more) {
-        st.template land<true>(kh, lk + (at ^ kTile));
-        st.template land<false>(vh, lv + (at ^ kTile));
-      }
-      wait_loads();
-      meet();
-    }
   }
   w.finish(a, row, a.part_o != nullptr, prefix ? a.own_splits + split : split,
            a.own_splits + a.prefix_splits);
@@ -1112,40 +1088,31 @@ struct Narrow {
     return __any(bad);
   }
 
-  // values() where V holds infinities or NaN that some rows do not see (see
-  // Wave::values_seen).
+  // values() where V holds infinities or NaN that some rows do not see: one
+  // key's product at a time, kept by the rows that see the key.
   __device__ __forceinline__ void values_seen(uint32_t at, const f32x4 (&s)[QT][kSub], const int (&seen)[QT]) {
-    const int g4 = ((threadIdx.x >> 4) & 3) * 4;
-    constexpr int kN = KEYS == 16 ? 4 : 8;
-    constexpr uint16_t one = 0x3F80;
+    const uint32_t g = (threadIdx.x >> 4) & 3;
+    constexpr int kWords = KEYS / 8;
+    typedef uint32_t words __attribute__((ext_vector_type(kWords)));
+#pragma unroll 1
+    for (uint32_t key = 0; key < KEYS; ++key) {
+      // the key's element of an operand: lanes of group key / 4 % 4, place key / 16 * 4 + key % 4
+      const uint32_t place = key / 16 * 4 + key % 4;
+      const uint32_t half = (key / 4 & 3) == g ? 0xFFFFu << (place & 1) * 16 : 0;
+      words only;
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) {
-      const auto v = v_operand(at, j);
-      typedef uint16_t u16xn __attribute__((ext_vector_type(kN)));
-      const u16xn w = __builtin_bit_cast(u16xn, v);
-      u16xn fine, high, low;
-#pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        const bool bad = (w[i] & 0x7F80) == 0x7F80;
-        fine[i] = bad ? (uint16_t)0 : w[i];
-        high[i] = bad && w[i] != 0xFF80 ? one : (uint16_t)0;
-        low[i] = bad && w[i] != 0x7F80 ? one : (uint16_t)0;
-      }
+      for (int i = 0; i < kWords; ++i) only[i] = place / 2 == (uint32_t)i ? half : 0;
 #pragma unroll
       for (int c = 0; c < QT; ++c) {
-        u16xn sees;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) sees[i] = 16 * (i / 4) + i % 4 < seen[c] - g4 ? one : (uint16_t)0;
         const auto p = p_operand(s[c]);
-        using V = decltype(v);
-        const V y = __builtin_bit_cast(V, sees);
-        o[c][j] = multiply(__builtin_bit_cast(V, fine), p, o[c][j]);
-        const f32x4 up = multiply(__builtin_bit_cast(V, high), y, f32x4{});
-        const f32x4 down = multiply(__builtin_bit_cast(V, low), y, f32x4{});
+        using V = decltype(v_operand(at, 0));
+        const V weight = __builtin_bit_cast(V, __builtin_bit_cast(words, p) & only);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (up[r] > 0) o[c][j][r] += __builtin_inff();
-          if (down[r] > 0) o[c][j][r] -= __builtin_inff();
+        for (int j = 0; j < D / 16; ++j) {
+          const V v = __builtin_bit_cast(V, __builtin_bit_cast(words, v_operand(at, j)) & only);
+          const f32x4 with = multiply(v, weight, o[c][j]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[c][j][r] = (int)key < seen[c] ? with[r] : o[c][j][r];
         }
       }
     }

@@ -11,12 +11,20 @@ nothing waits for the GPU.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from . import claimkv
-from .claimkv import CAttendDesc, CKvDesc, CRows, CSeqs, ENOSPC, _check, _device_ints, _torch, lib
+from .claimkv import CAttendDesc, CKvDesc, CRows, CSeqs, ENOSPC, OK, _check, _torch, lib
 
 SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED = 0, 1, 2
 NONE = -1  # a table entry that names no block (0xFFFFFFFF in 32 bits)
+
+# claim_kv_desc with two claim_rows after it, and claim_attend_desc, packed in
+# one step: filling them field by field takes longer than queueing the work
+_WRITE = struct.Struct("<4I2Q2f6Q")
+_ATTEND = struct.Struct("<4I2Q2f6Q2IQfI2Q")
+assert _WRITE.size == ctypes.sizeof(CKvDesc) + 2 * ctypes.sizeof(CRows)
+assert _ATTEND.size == ctypes.sizeof(CAttendDesc)
 
 
 class Sequences:
@@ -40,7 +48,7 @@ class Sequences:
             lengths = torch.zeros(tables.shape[0], dtype=torch.int32, device=dev)
         if refs is None:
             refs = torch.zeros(g.num_blocks, dtype=torch.int32, device=dev)
-        _device_ints(dev, tables=tables, lengths=lengths, refs=refs)
+        claimkv._device_ints(dev, tables=tables, lengths=lengths, refs=refs)
         if lengths.numel() != tables.shape[0] or refs.numel() != g.num_blocks:
             raise ValueError("lengths needs one entry per sequence, refs one per block")
         self.pool, self.tables, self.lengths, self.refs = pool, tables, lengths, refs
@@ -51,43 +59,40 @@ class Sequences:
                            refs=refs.data_ptr(), work=self._scratch.data_ptr())
         self._seqs_ref = ctypes.addressof(self._seqs)
         self._state = (tables, lengths, refs, self._scratch)
-        self._work = None
+        self._work, self._work_at, self._work_bytes = None, 0, 0
+        self._desc = ctypes.create_string_buffer(_ATTEND.size)
+        self._desc_at = ctypes.addressof(self._desc)
+        self._device, self._bf16, self._int32 = dev, torch.bfloat16, torch.int32
+        self._heads, self._dim = g.num_kv_heads, g.head_dim
 
     # ------------------------------------------------------------- blocks
     def grow(self, ids, tokens):
         """claim_seqs_grow: ``tokens[i]`` more tokens for sequence ``ids[i]``
         (None: sequences 0..n-1), with blocks for them.  Returns the device
         tensor of statuses (SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED)."""
-        return self._entries(lib().claim_seqs_grow, "claim_seqs_grow", ids=ids, tokens=tokens)
+        at = 0 if ids is None else self._ints("ids", ids)
+        return self._entries(lib().claim_seqs_grow, "claim_seqs_grow", ids, at, "tokens", tokens)
 
     def fork(self, parents, children):
         """claim_seqs_fork: the empty sequence ``children[i]`` becomes a copy
         of ``parents[i]`` that shares its full blocks.  Returns the statuses."""
-        return self._entries(lib().claim_seqs_fork, "claim_seqs_fork", parents=parents,
-                             children=children)
+        at = self._ints("parents", parents)
+        return self._entries(lib().claim_seqs_fork, "claim_seqs_fork", parents, at, "children", children)
 
-    def _entries(self, call, what, **given):
-        (name, first), (_, second) = given.items()
-        pool = self.pool
-        _device_ints(pool.kv.device, **given)
-        if first is None and name != "ids" or second is None:
-            raise ValueError(f"{what} needs {' and '.join(given)}")
-        n = second.numel()
+    def _entries(self, call, what, first, first_at, name, second):
+        pool, second_at, n = self.pool, self._ints(name, second), second.numel()
         if first is not None and first.numel() != n:
-            raise ValueError(f"{' and '.join(given)} need one entry per sequence")
+            raise ValueError(f"{what} needs as many {name}")
         status = second.new_empty(n)
         with pool.ordered(first, second, status, *self._state):
-            _check(call(pool._h, self._seqs_ref, _ptr(first), second.data_ptr(), n,
-                        status.data_ptr()), what)
+            _check(call(pool._h, self._seqs_ref, first_at, second_at, n, status.data_ptr()), what)
         return status
 
     def free(self, ids) -> None:
         """claim_seqs_free: sequences ``ids`` give up their blocks."""
-        pool = self.pool
-        _device_ints(pool.kv.device, ids=ids)
+        pool, at = self.pool, self._ints("ids", ids)
         with pool.ordered(ids, *self._state):
-            _check(lib().claim_seqs_free(pool._h, self._seqs_ref, ids.data_ptr(), ids.numel()),
-                   "claim_seqs_free")
+            _check(lib().claim_seqs_free(pool._h, self._seqs_ref, at, ids.numel()), "claim_seqs_free")
 
     def compact(self):
         """claim_seqs_compact: blocks in use move to the front of the pool.
@@ -106,15 +111,14 @@ class Sequences:
         head_dim], bf16) become the last tokens of their sequences in
         ``layer``: rows offsets[s]..offsets[s + 1] of sequence ids[s] (without
         ``offsets``, row s alone; without ``ids``, sequence s)."""
-        pool, g = self.pool, self.pool.geometry
-        heads, dim = g.num_kv_heads, g.head_dim
-        rows_k, rows_v = self._rows("k", k, heads, dim), self._rows("v", v, heads, dim)
-        if k.shape[0] != v.shape[0]:
+        pool, rows = self.pool, k.shape[0]
+        if rows != v.shape[0]:
             raise ValueError("k and v need the same rows")
-        kv = self._kv(layer, k.shape[0], ids, offsets, k_scale, v_scale)
+        _WRITE.pack_into(self._desc, 0, *self._kv(layer, rows, ids, offsets), k_scale, v_scale,
+                         *self._rows("k", k, self._heads), *self._rows("v", v, self._heads))
+        at = self._desc_at
         with pool.ordered(k, v, ids, offsets, *self._state):
-            _check(lib().claim_kv_write(pool._h, self._seqs_ref, ctypes.addressof(kv),
-                                        ctypes.addressof(rows_k), ctypes.addressof(rows_v)),
+            _check(lib().claim_kv_write(pool._h, self._seqs_ref, at, at + 40, at + 64),
                    "claim_kv_write")
 
     def attend(self, layer: int, q, *, ids=None, offsets=None, scale: float | None = None,
@@ -122,8 +126,11 @@ class Sequences:
         """claim_attend: causal attention of ``q`` ([rows, heads, head_dim],
         bf16) over their sequences' tokens in ``layer``, the rows being the
         sequences' last tokens (as in :meth:`write`, which comes first).
-        ``scale`` defaults to head_dim ** -0.5.  Returns ``out``."""
-        return self._attend(layer, q, None, ids, offsets, scale, k_scale, v_scale, out)
+        ``scale`` defaults to head_dim ** -0.5.  Returns ``out``.
+
+        The first call of a shape allocates scratch (so it comes before a
+        graph capture of that shape); later ones use it again."""
+        return self._attend(layer, q, None, 0, 0, ids, offsets, scale, k_scale, v_scale, out)
 
     def attend_shared(self, layer: int, q, prefix, *, ids=None, offsets=None,
                       scale: float | None = None, k_scale: float = 1.0, v_scale: float = 1.0,
@@ -131,60 +138,66 @@ class Sequences:
         """:meth:`attend` for sequences that all begin with the whole blocks
         ``prefix`` (int32 device tensor), which are read once for all of them;
         the tables' own entries for those positions are not read."""
-        _device_ints(self.pool.kv.device, prefix=prefix)
-        return self._attend(layer, q, prefix, ids, offsets, scale, k_scale, v_scale, out)
+        return self._attend(layer, q, prefix, self._ints("prefix", prefix), prefix.numel(), ids,
+                            offsets, scale, k_scale, v_scale, out)
 
-    def _attend(self, layer, q, prefix, ids, offsets, scale, k_scale, v_scale, out):
+    def _attend(self, layer, q, prefix, prefix_at, blocks, ids, offsets, scale, k_scale, v_scale, out):
         torch = _torch()
-        pool, dim = self.pool, self.pool.geometry.head_dim
-        heads = q.shape[1] if q.dim() == 3 else 0
+        pool, shape = self.pool, q.shape
+        if len(shape) != 3:
+            raise ValueError("q must be [rows, heads, head_dim]")
+        heads = shape[1]
+        rows_q = self._rows("q", q, heads)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        d = CAttendDesc(kv=self._kv(layer, q.shape[0], ids, offsets, k_scale, v_scale),
-                        q=self._rows("q", q, heads, dim), out=self._rows("out", out, heads, dim),
-                        num_heads=heads, prefix_blocks=0 if prefix is None else prefix.numel(),
-                        prefix=_ptr(prefix), scale=dim**-0.5 if scale is None else scale)
-        if out.shape != q.shape:
+            out = torch.empty(shape, dtype=self._bf16, device=self._device)
+        elif out.shape != shape:
             raise ValueError("out needs q's shape")
-        at = ctypes.addressof(d)
+        given = (*self._kv(layer, shape[0], ids, offsets), k_scale, v_scale, *rows_q,
+                 *self._rows("out", out, heads), heads, blocks, prefix_at,
+                 self._dim**-0.5 if scale is None else scale, 0)
+        _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
         with pool.ordered(q, out, ids, offsets, prefix, pool.kv, *self._state):
-            if self._work is not None:
-                d.work, d.work_bytes = self._work.data_ptr(), self._work.numel()
-            rc = lib().claim_attend(pool._h, self._seqs_ref, at)
+            rc = lib().claim_attend(pool._h, self._seqs_ref, self._desc_at)
             if rc == ENOSPC:  # the first call of a larger shape
                 need = ctypes.c_uint64()
-                _check(lib().claim_attend_work(pool._h, self._seqs_ref, at, ctypes.byref(need)),
-                       "claim_attend_work")
+                _check(lib().claim_attend_work(pool._h, self._seqs_ref, self._desc_at,
+                                               ctypes.byref(need)), "claim_attend_work")
                 # memory of the pool's stream: what was queued there may use
                 # the smaller one until it is done
                 with torch.cuda.stream(pool.stream):
-                    self._work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-                d.work, d.work_bytes = self._work.data_ptr(), need.value
-                rc = lib().claim_attend(pool._h, self._seqs_ref, at)
-            _check(rc, "claim_attend")
+                    self._work = torch.empty(need.value, dtype=torch.uint8, device=self._device)
+                self._work_at, self._work_bytes = self._work.data_ptr(), need.value
+                _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
+                rc = lib().claim_attend(pool._h, self._seqs_ref, self._desc_at)
+            if rc != OK:
+                _check(rc, "claim_attend")
         return out
 
-    def _kv(self, layer, rows, ids, offsets, k_scale, v_scale) -> CKvDesc:
-        _device_ints(self.pool.kv.device, ids=ids, offsets=offsets)
+    # ------------------------------------------------------------ checks
+    def _ints(self, name, t) -> int:
+        """The address of a contiguous int32 tensor on the pool's device."""
+        if t.dtype != self._int32 or t.device != self._device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor on {self._device}")
+        return t.data_ptr()
+
+    def _kv(self, layer, rows, ids, offsets):
+        """claim_kv_desc up to the scales."""
+        n, ids_at, offsets_at = rows, 0, 0
         if offsets is not None:
-            n = offsets.numel() - 1
-        else:
-            n = rows
-        if n < 0 or ids is not None and ids.numel() != n:
-            raise ValueError("ids needs one entry per sequence, offsets one more")
-        if layer < 0:
-            raise ValueError("layer must not be negative")
-        return CKvDesc(layer=layer, num_seqs=n, num_rows=rows, ids=_ptr(ids), offsets=_ptr(offsets),
-                       k_scale=k_scale, v_scale=v_scale)
+            offsets_at, n = self._ints("offsets", offsets), offsets.numel() - 1
+        if ids is not None:
+            ids_at = self._ints("ids", ids)
+            if ids.numel() != n:
+                raise ValueError("ids needs one entry per sequence")
+        if n < 0 or layer < 0:
+            raise ValueError("offsets needs one entry more than sequences; layer must not be negative")
+        return layer, n, rows, 0, ids_at, offsets_at
 
-    def _rows(self, name, x, heads, dim) -> CRows:
-        torch = _torch()
-        if (x.dtype != torch.bfloat16 or x.device != self.pool.kv.device or x.dim() != 3
-                or x.shape[1:] != (heads, dim) or x.numel() and x.stride(2) != 1):
-            raise ValueError(f"{name} must be bf16 [rows, {heads}, {dim}] on {self.pool.kv.device}, "
+    def _rows(self, name, x, heads):
+        """claim_rows."""
+        stride, dim = x.stride(), self._dim
+        if (x.dtype != self._bf16 or x.device != self._device or len(stride) != 3
+                or x.shape[1] != heads or x.shape[2] != dim or stride[2] != 1):
+            raise ValueError(f"{name} must be bf16 [rows, {heads}, {dim}] on {self._device}, "
                              "its last dimension contiguous")
-        return CRows(data=x.data_ptr(), row_stride=x.stride(0), head_stride=x.stride(1))
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+        return x.data_ptr(), stride[0], stride[1]
