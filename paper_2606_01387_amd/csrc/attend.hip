@@ -736,6 +736,16 @@ __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// The weights are made here, whatever the compiler thinks of later places.
+__device__ __forceinline__ void hold(bf16x8 (&p)[2][2]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u32x4 w = __builtin_bit_cast(u32x4, p[i / 2][i % 2]);
+    asm volatile("" : "+v"(w));
+    p[i / 2][i % 2] = __builtin_bit_cast(bf16x8, w);
+  }
+}
+
 // How many of the `keys` positions from `pos` on the row sees.
 __device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys) {
   return r.limit <= pos ? 0 : r.limit - pos < keys ? (int)(r.limit - pos) : (int)keys;
@@ -752,15 +762,15 @@ __device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys
 // some row does not see in full come last, one after another.
 //
 // In wave terms: M(n) reads tile n of K and n - 1 of V, W(n) makes weights of
-// tile n and copies tile n + A of K and n + A - 1 of V (A = 2; e4m3 3, since
-// its bytes stop in registers and land in W(n + 1)).  A ring of A + 1 tiles: the
-// one that W(n) fills was last read in M(n - 1), by every wave before any is in
-// W(n).  bf16 copies are waited for at the end of M(n + 1), one barrier before
-// the first wave is in M(n + 2).
+// tile n and asks for tile n + 3 of K and n + 2 of V.  bf16 copies go to LDS and
+// are waited for at the end of W(n + 1); e4m3 bytes stop in registers and land
+// in W(n + 1).  A ring of four tiles: what W(n) fills was last read in M(n - 1),
+// by every wave before any is in W(n), and is read first in M(n + 3), after a
+// barrier that every wave reaches with its copies done.
 
 template <int D, bool E4M3, int WAVES, bool ONE>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
-  constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2, kAhead = E4M3 ? 3 : 2;
+  constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2, kAhead = 3;
   using St = Stage<D * (E4M3 ? 1 : 2), E4M3, kKeys, WAVES * 64, ONE, WideSwizzle<D>>;
   __shared__ __align__(1024) uint8_t lk[(kAhead + 1) * kTile];
   __shared__ __align__(1024) uint8_t lv[(kAhead + 1) * kTile];
@@ -787,7 +797,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
     return from < hi ? hi - from : 0;
   };
   // copies begin before anything else: tiles 0 and 1 of K and 0 of V, then
-  // what W(-1) would have asked for
+  // what W(-1) would have asked for, 2 of K and 1 of V
   {
     typename St::Rows ahead[kAhead];
     typename St::Held first[2];
@@ -807,12 +817,10 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
     st.template land<true>(first[0], lk);
     st.template land<false>(vh, lv);
     st.template land<true>(first[1], lk + kTile);
-    if (E4M3) {
-      vp = kp;
-      kp = st.place(a, ahead[kAhead - 1], left(2));
-      st.template issue<true>(k, kp, lk, kh);
-      st.template issue<false>(v, vp, lv, vh);
-    }
+    vp = kp;
+    kp = st.place(a, ahead[2], left(2));
+    st.template issue<true>(k, kp, lk + 2 * kTile, kh);
+    st.template issue<false>(v, vp, lv + kTile, vh);
   }
   const Row row = row_at(a, it, (t >> 6) * 32 + (t & 31));
   Wave<D> w;
@@ -831,8 +839,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   uint32_t now = 0, n = 0;  // tile n is at `now` in the ring
   const auto before = [&](uint32_t x) { return x ? x - kTile : kAhead * kTile; };
   const auto fetch = [&] {
-    const uint32_t to = before(now);  // tile n + A of K takes the place of n - 1
-    if (E4M3) {  // what W(n - 1) asked for: tile n + A - 1 of K, n + A - 2 of V
+    const uint32_t to = before(now);  // tile n + 3 of K takes the place of n - 1
+    if (E4M3) {  // what W(n - 1) asked for: tile n + 2 of K, n + 1 of V
       st.template land<true>(kh, lk + before(to));
       st.template land<false>(vh, lv + before(before(to)));
     }
@@ -855,6 +863,9 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
       fetch();
       w.template weights<2>(a, s, p);
       step();
+      // all but what was asked for just now; and no work moves behind the barrier
+      if (!E4M3) wait_copies<2 * St::kSteps>();
+      hold(p);
       meet();
     };
     w.template scores<2>(lk, s);
@@ -865,7 +876,6 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
       __builtin_amdgcn_s_setprio(1);
       w.multiply(lv + before(now), p, lk + now, s);
       __builtin_amdgcn_s_setprio(0);
-      if (!E4M3) wait_loads();
       meet();
       weigh();
     }
