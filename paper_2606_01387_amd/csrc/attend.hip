@@ -322,6 +322,28 @@ struct Stage {
   }
 };
 
+// Everything that this wave has asked memory for has arrived.
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
+}
+
+// All but the last N copies to LDS have arrived.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N < 64, "");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0F70);
+  asm volatile("" ::: "memory");
+}
+
+// This wave's LDS reads and writes are done.
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+}
+
 // ------------------------------------------------------- one wave's 32 rows
 
 __device__ __forceinline__ float across_halves_max(float x) {
@@ -522,25 +544,39 @@ struct Wave {
     }
   }
 
-  // The rows' results, or their parts for the joining kernel.
-  __device__ __forceinline__ void finish(const Args& a, const Row& r, bool parts, uint32_t split,
-                                         uint32_t splits) {
+  // The rows' parts for the joining kernel: through LDS of the wave's own (32
+  // rows of D floats), so that whole rows are stored at a time.
+  __device__ __forceinline__ void finish_part(const Args& a, const Row& r, uint32_t split, uint32_t splits,
+                                              uint8_t* lds) {
+    const uint32_t lane = threadIdx.x & 63, h = lane >> 5, row = lane & 31;
+    const float sum = across_halves_add(l);
+    uint64_t at = ((uint64_t)r.row * a.heads * a.group + r.head) * splits + split;
+    if (r.valid && h == 0) a.part_ml[at] = float2{m, sum};
+    if (!r.valid || sum == 0.0f) at = ~0ull;
+    constexpr uint32_t kChunks = D / 4;  // 16-byte chunks of a row, exchanged by its number
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const uint32_t chunk = (8 * j + 2 * g + h) ^ (row & (kChunks - 1));
+        *(f32x4*)(lds + (row * kChunks + chunk) * 16) =
+            f32x4{o[j][4 * g], o[j][4 * g + 1], o[j][4 * g + 2], o[j][4 * g + 3]};
+      }
+    wait_lds();
+#pragma unroll
+    for (uint32_t i = 0; i < 32 * kChunks / 64; ++i) {
+      const uint32_t x = i * 64 + lane, from = x / kChunks, chunk = x % kChunks;
+      const f32x4 w = *(const f32x4*)(lds + (from * kChunks + (chunk ^ (from & (kChunks - 1)))) * 16);
+      const uint64_t to = (uint64_t)__shfl((uint32_t)(at >> 32), from) << 32 | __shfl((uint32_t)at, from);
+      if (to != ~0ull) *(f32x4*)(a.part_o + to * D + chunk * 4) = w;
+    }
+  }
+
+  // The rows' results.
+  __device__ __forceinline__ void finish(const Args& a, const Row& r) {
     const uint32_t h = (threadIdx.x >> 5) & 1;
     const float sum = across_halves_add(l);
     if (!r.valid) return;
-    if (parts) {
-      const uint64_t at = ((uint64_t)r.row * a.heads * a.group + r.head) * splits + split;
-      if (h == 0) a.part_ml[at] = float2{m, sum};
-      if (sum == 0.0f) return;
-      float* dst = a.part_o + at * D + 4 * h;
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *(f32x4*)(dst + 32 * j + 8 * g) =
-              f32x4{o[j][4 * g], o[j][4 * g + 1], o[j][4 * g + 2], o[j][4 * g + 3]};
-      return;
-    }
     const float f = sum == 0.0f ? 0.0f : a.v_scale / sum;
     uint16_t* dst = a.out + r.row * a.out_row + r.head * a.out_head + 4 * h;
 #pragma unroll
@@ -706,28 +742,6 @@ __device__ __forceinline__ void seen_by_wave(const Row& row, int lanes, uint32_t
   *least = uniform(lo);
 }
 
-// Everything that this wave has asked memory for has arrived.
-__device__ __forceinline__ void wait_loads() {
-  __builtin_amdgcn_s_waitcnt(0);
-  asm volatile("" ::: "memory");
-}
-
-// All but the last N copies to LDS have arrived.
-template <int N>
-__device__ __forceinline__ void wait_copies() {
-  static_assert(N < 64, "");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0F70);
-  asm volatile("" ::: "memory");
-}
-
-// This wave's LDS reads and writes are done.
-__device__ __forceinline__ void wait_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);
-  asm volatile("" ::: "memory");
-}
-
 __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);  // no work of one phase moves into the other
   wait_lds();
@@ -873,9 +887,9 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
     weigh();
 #pragma unroll 1
     while (n < full) {
-      __builtin_amdgcn_s_setprio(1);
-      w.multiply(lv + before(now), p, lk + now, s);
       __builtin_amdgcn_s_setprio(0);
+      w.multiply(lv + before(now), p, lk + now, s);
+      __builtin_amdgcn_s_setprio(1);
       meet();
       weigh();
     }
@@ -894,8 +908,16 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
     wait_loads();
     meet();
   }
-  w.finish(a, row, a.part_o != nullptr, prefix ? a.own_splits + split : split,
-           a.own_splits + a.prefix_splits);
+  if (a.part_o) {
+    meet();  // the tiles have been read
+    constexpr uint32_t kRoom = 32 * D * 4;
+    static_assert(WAVES / 2 * kRoom <= 4 * kTile, "");
+    const uint32_t wave = uniform(t >> 6);
+    w.finish_part(a, row, prefix ? a.own_splits + split : split, a.own_splits + a.prefix_splits,
+                  wave < WAVES / 2 ? lk + wave * kRoom : lv + (wave - WAVES / 2) * kRoom);
+  } else {
+    w.finish(a, row);
+  }
 }
 
 // ------------------------------------------------------------ few query rows
