@@ -922,8 +922,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
 
 // ------------------------------------------------------------ few query rows
 //
-// QT x 16 query rows of one sequence, as columns of 16 x 16 products, against a
-// long axis of keys.
+// QT x 16 query rows, as columns of 16 x 16 products, against a long axis of
+// keys: the rows of one decoding sequence, or of many that share a prefix.
 // Four waves hold the same rows and take every fourth group of KEYS keys
 // through LDS of their own, so no wave waits for another until their parts
 // are joined at the end.  K and V have two places each; the copy into one
@@ -1151,26 +1151,34 @@ struct Narrow {
   }
 };
 
-template <int D, bool E4M3, bool ONE, int QT>
+template <int D, bool E4M3>
 struct Few {
   static constexpr int kWaves = 4, kBytes = D * (E4M3 ? 1 : 2);
   static constexpr int kKeys = kBytes == 256 ? 16 : 32;  // LDS for two workgroups on a CU
   static constexpr int kTile = kKeys * kBytes;
-  static constexpr int kLds = kWaves * 4 * kTile;
+  static constexpr int kRing = kWaves * 4 * kTile;
+  static constexpr int kRows = 32;  // at most
+  struct Lds {
+    __align__(1024) uint8_t ring[kRing];
+    float tops[kWaves][kRows], sums[kWaves][kRows];
+  };
 };
 
 template <int D, bool E4M3, bool ONE, int QT>
-__global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
-  using F = Few<D, E4M3, ONE, QT>;
+__device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
+                                         typename Few<D, E4M3>::Lds& shared) {
+  using F = Few<D, E4M3>;
   constexpr int M = 16 * QT, kKeys = F::kKeys, kTile = F::kTile, kWaves = F::kWaves;
   using St = Stage<F::kBytes, false, kKeys, 64, ONE, NarrowSwizzle<F::kBytes>>;
-  __shared__ __align__(1024) uint8_t lds[F::kLds];
+  uint8_t* const lds = shared.ring;
+  auto& tops = shared.tops;
+  auto& sums = shared.sums;
   const uint32_t wave = uniform(threadIdx.x >> 6), t = threadIdx.x & 63;
-  uint32_t b = blockIdx.x;
   const uint32_t kv_head = b % a.heads;
   b /= a.heads;
-  const uint32_t split = b % a.own_splits, tile = b / a.own_splits;
-  const Tile it = make_tile<M>(a, false, tile, split, a.own_splits, kv_head, kKeys);
+  const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
+  const uint32_t split = b % splits, tile = b / splits;
+  const Tile it = make_tile<M>(a, prefix, tile, split, splits, kv_head, kKeys);
   if (!it.any) return;
   Row row[QT];
   uint32_t least = ~0u;
@@ -1219,8 +1227,6 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
 #pragma unroll
       for (int c = 0; c < QT; ++c) seen[c] = masked ? seen_of(row[c], pos, kKeys) : kKeys;
       at = st.place(a, rows, rest(pos + 2 * kStep));
-      st.next(a, add_blocks, add_tokens, rows);
-      st.look(it.range, rows);
       wait_copies<kLater>();
       w.scores(lk + x, s);
       wait_lds();
@@ -1228,6 +1234,11 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
       w.weights(a, s, masked, seen);
       wait_copies<kLater>();
       w.values(lv + x, s, masked, seen);
+      // table entries are read where the products of V hide it: scalar loads
+      // and LDS reads share a counter
+      __builtin_amdgcn_sched_barrier(0);
+      st.next(a, add_blocks, add_tokens, rows);
+      st.look(it.range, rows);
       wait_lds();
       st.template issue<false>(v, at, lv + x, none);
     };
@@ -1242,7 +1253,6 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
     w.start(a, row);
   }
   // join the waves: each row's common maximum first, then two and two
-  __shared__ float tops[kWaves][M], sums[kWaves][M];
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
     if (t < 16) tops[wave][16 * c + t] = w.m[c];
@@ -1262,7 +1272,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
     for (int j = 0; j < D / 16; ++j) w.o[c][j] *= f;
   }
   constexpr uint32_t kPart = M * D;  // floats of one wave
-  static_assert(kPart * 4 * 2 <= F::kLds, "two waves' parts fit");
+  static_assert(kPart * 4 * 2 <= F::kRing, "two waves' parts fit");
   float* const parts = (float*)lds;
 #pragma unroll
   for (uint32_t half = kWaves / 2; half > 0; half /= 2) {
@@ -1291,7 +1301,8 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) w.l[c] += sums[i][16 * c + (t & 15)];
     if (a.part_o) {
-      const uint64_t to = ((uint64_t)row[c].row * a.heads * a.group + row[c].head) * all + split;
+      const uint64_t to = ((uint64_t)row[c].row * a.heads * a.group + row[c].head) * all +
+                          (prefix ? a.own_splits + split : split);
       if (t < 16) a.part_ml[to] = float2{w.m[c], w.l[c]};
       if (w.l[c] == 0.0f) continue;
 #pragma unroll
@@ -1309,6 +1320,25 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a) {
       }
     }
   }
+}
+
+// Items of a shared prefix (32 rows each) and of the sequences' own keys (16
+// QT rows) in one launch, eight of the one kind and eight of the other in
+// turn: the first are bound by products and weights, the second by memory, and
+// two workgroups share a CU.
+template <int D, bool E4M3, bool ONE, int QT>
+__global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_items, uint32_t own_items) {
+  __shared__ typename Few<D, E4M3>::Lds shared;
+  const uint32_t b = blockIdx.x, of8 = b / 8;
+  const uint32_t prefix8 = (prefix_items + 7) / 8, own8 = (own_items + 7) / 8;
+  const uint32_t both = prefix8 < own8 ? prefix8 : own8;
+  const bool prefix = of8 < 2 * both ? of8 % 2 == 0 : prefix8 > own8;
+  const uint32_t item = (of8 < 2 * both ? of8 / 2 : of8 - both) * 8 + b % 8;
+  if (item >= (prefix ? prefix_items : own_items)) return;
+  if (prefix)
+    few_rows<D, E4M3, ONE, 2>(a, true, item, shared);
+  else
+    few_rows<D, E4M3, ONE, QT>(a, false, item, shared);
 }
 
 // ------------------------------------------------------------------ joining
@@ -1375,11 +1405,13 @@ __global__ void __launch_bounds__(256) k_join(Args a) {
 
 struct Plan {
   uint32_t columns;  // own keys by k_attend_few with 16 x columns rows a tile; 0: by k_attend_rows
+  bool prefix_narrow;  // the prefix in k_attend_few's launch, else by k_attend_rows
   uint32_t own_splits, prefix_splits, tiles, prefix_tiles;
   uint64_t parts;  // parts of all rows and heads; 0: none are kept
 };
 
 constexpr uint32_t kRowsTile = 256;  // rows of k_attend_rows' tile
+constexpr uint32_t kPrefixTile = 32;  // of k_attend_few's, for a prefix
 // Splits of `keys` for `groups` workgroups where `slots` run at a time: all of
 // them in one round, no share shorter than `least` keys.
 uint32_t splits_for(uint64_t groups, uint64_t slots, uint64_t keys, uint64_t least) {
@@ -1401,8 +1433,14 @@ Plan make_plan(const PoolView& p, const claim_seqs* s, const claim_attend_desc* 
   r.own_splits = splits_for((uint64_t)r.tiles * p.heads, r.columns ? 2ull * p.cus : p.cus, own,
                             r.columns ? 256 : 512);
   if (prefix) {
-    r.prefix_tiles = (uint32_t)((rows * group + kRowsTile - 1) / kRowsTile);
-    r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, p.cus, prefix, 256);
+    // few_rows makes 0.3 M (query row, key) pairs a microsecond beside the own
+    // keys and in their launch; k_attend_rows makes 2.4 M after 14 us, in a launch
+    // of its own.  8192 shared tokens, 8 KV heads, 4 query heads each, 4 / 16 / 64
+    // sequences: 22 / 32 / 65 us and 31 / 32 / 40 us.
+    r.prefix_narrow = r.columns && rows * d->num_heads * prefix <= (8u << 20);
+    const uint32_t tile = r.prefix_narrow ? kPrefixTile : kRowsTile;
+    r.prefix_tiles = (uint32_t)((rows * group + tile - 1) / tile);
+    r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, (r.prefix_narrow ? 2ull : 1ull) * p.cus, prefix, 256);
   }
   const uint64_t splits = (uint64_t)r.own_splits + r.prefix_splits;
   r.parts = splits > 1 ? rows * d->num_heads * splits : 0;
@@ -1429,17 +1467,18 @@ int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc
 template <int D, bool E4M3, bool ONE>
 int launch_one(const PoolView& p, const Plan& plan, const Args& a) {
   constexpr int kWaves = kRowsTile / 32;
-  const dim3 own(plan.tiles * a.heads * a.own_splits);
-  switch (plan.columns) {
-    case 1: hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 1>), own, dim3(256), 0, p.stream, a); break;
-    case 2: hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 2>), own, dim3(256), 0, p.stream, a); break;
-    default:
-      hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>), own, dim3(kWaves * 64), 0, p.stream, a, 0u);
-  }
-  if (plan.prefix_tiles)
-    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>),
-                       dim3(plan.prefix_tiles * a.heads * a.prefix_splits), dim3(kWaves * 64), 0,
-                       p.stream, a, 1u);
+  const uint32_t own = plan.tiles * a.heads * a.own_splits;
+  const uint32_t prefix = plan.prefix_tiles * a.heads * a.prefix_splits;
+  const uint32_t narrow = plan.prefix_narrow ? prefix : 0;
+  const dim3 both((own + 7) / 8 * 8 + (narrow + 7) / 8 * 8), rows(kWaves * 64);
+  if (plan.columns == 1)
+    hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 1>), both, dim3(256), 0, p.stream, a, narrow, own);
+  else if (plan.columns == 2)
+    hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 2>), both, dim3(256), 0, p.stream, a, narrow, own);
+  else
+    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>), dim3(own), rows, 0, p.stream, a, 0u);
+  if (prefix > narrow)
+    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>), dim3(prefix), rows, 0, p.stream, a, 1u);
   if (plan.parts)
     hipLaunchKernelGGL((k_join<D>), dim3((a.rows * a.heads * a.group + 3) / 4), dim3(256), 0, p.stream, a);
   return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;
