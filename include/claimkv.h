@@ -582,7 +582,7 @@ typedef struct claim_rows {
  * last ones: with n rows and length L, row i of it is position L - n + i.
  * Layer l of a pool of K and V planes (planes_per_layer = 2) is meant.  A
  * pool with elem_bytes 2 holds bf16, with elem_bytes 1 e4m3: a byte times
- * k_scale or v_scale is the value (both must be finite and > 0; bf16 pools
+ * k_scale or v_scale is the value (both between 1e-30 and 1e30; bf16 pools
  * take 1). */
 typedef struct claim_kv_desc {
   uint32_t layer;

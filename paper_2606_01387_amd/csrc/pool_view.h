@@ -31,6 +31,9 @@ inline int check_seqs(const claim_seqs* s) {
 
 inline bool finite_positive(float x) { return x > 0.0f && x <= 3.4e38f; }
 
+// A scale of e4m3 bytes: its inverse and its product with a byte are finite.
+inline bool scale_ok(float x) { return x >= 1e-30f && x <= 1e30f; }
+
 inline int check_kv(const PoolView& p, const claim_seqs* s, const claim_kv_desc* kv) {
   if (kv->reserved != 0 || p.planes_per_layer != 2 || kv->layer >= p.layers ||
       (p.elem != 1 && p.elem != 2) || kv->num_seqs > s->max_seqs || kv->num_rows > 0x7FFFFFFFu)
@@ -38,7 +41,7 @@ inline int check_kv(const PoolView& p, const claim_seqs* s, const claim_kv_desc*
   if (!kv->offsets && kv->num_rows != kv->num_seqs) return CLAIM_EINVAL;
   if (kv->num_rows > 0 && kv->num_seqs == 0) return CLAIM_EINVAL;
   if (p.elem == 2 ? kv->k_scale != 1.0f || kv->v_scale != 1.0f
-                  : !finite_positive(kv->k_scale) || !finite_positive(kv->v_scale))
+                  : !scale_ok(kv->k_scale) || !scale_ok(kv->v_scale))
     return CLAIM_EINVAL;
   return CLAIM_OK;
 }
