@@ -446,6 +446,8 @@ struct Wave {
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
+        // the sum takes the weight before it is rounded: the rounded one costs
+        // 6 % of the kernel's time, for an error of 2.1e-3 in place of 2.2e-3
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], a.c, -mc));
         sum[r & 1] += e;
         p[u][r / 8][r % 8] = (__bf16)e;
@@ -1036,7 +1038,9 @@ struct Narrow {
       for (int n = 0; n < kSub; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[c][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], a.c, -mc));
+          // the weight that is summed is the rounded one that multiplies V:
+          // what rounding does to a row's heaviest weights divides out again
+          s[c][n][r] = (float)(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], a.c, -mc));
           l[c] += s[c][n][r];
         }
     }
