@@ -177,58 +177,66 @@ __device__ __forceinline__ u32x4 widen(uint32_t a, uint32_t b) {
 // straight to LDS; or (WIDEN) e4m3 rows into registers by issue(), and widened
 // to bf16 into LDS by land().
 //
-// ONE: the rows that a wave loads with one instruction (4 of 256 bytes to 16
-// of 64) lie in one block, as they do wherever their number divides the block
-// size.  Block, token and address are then the wave's, on the scalar unit;
-// otherwise each lane has its own.  16384 causal tokens, 32 heads over 8 of
-// 128, blocks of 16: FIGURE-ONE.
-template <int BYTES, bool WIDEN, int KEYS, int THREADS, bool ONE, typename Swizzle>
+// WITHIN says which rows surely lie in one block of the cache, so that they
+// share a table entry and a base address on the scalar unit: those of one
+// load instruction of a wave (4 of 256 bytes to 16 of 64: their number divides
+// the block size), or all of a wave's tile (KEYS divides it); otherwise each
+// lane has its own.  16384 causal tokens, 32 heads over 8 of 128, blocks of 16:
+// 2.40 ms with lanes of their own, 2.01 ms with loads.
+enum Within : int { kLanes = 0, kLoads = 1, kTiles = 2 };
+
+template <int BYTES, bool WIDEN, int KEYS, int THREADS, Within WITHIN, typename Swizzle>
 struct Stage {
   static constexpr int kRowLanes = BYTES / 16;  // lanes of one row
   static constexpr int kWaveRows = 64 / kRowLanes;
   static constexpr int kRows = THREADS / kRowLanes;  // rows of one step
   static constexpr int kSteps = KEYS / kRows ? KEYS / kRows : 1;
+  static constexpr int kLooks = WITHIN == kTiles ? 1 : kSteps;  // table entries of a tile
+  static constexpr bool kScalar = WITHIN != kLanes;
   static_assert(WIDEN || KEYS % kRows == 0, "tiles are filled by whole steps");
+  static_assert(WITHIN != kTiles || (THREADS == 64 && !WIDEN), "a wave's own tile");
 
   struct Held {  // e4m3 bytes on their way
     u32x4 r[WIDEN ? kSteps : 1];
   };
 
-  // The rows of one tile, a wave's first of each step (ONE) or a lane's own:
-  // where they are in the list of blocks, and its entries once they are read.
+  // The rows of one tile, a wave's first of each look or a lane's own: where
+  // they are in the list of blocks, and its entries once they are read.
   struct Rows {
-    uint32_t at[kSteps], token[kSteps], entry[kSteps];
+    uint32_t at[kLooks], token[kLooks], entry[kLooks];
   };
 
   // Where they are in a plane.
   struct Places {
-    uint64_t byte[kSteps];
-    uint32_t entry[kSteps];
+    uint64_t byte[kLooks];
+    uint32_t entry[kLooks];
     uint32_t left;  // rows of the tile that the range has
   };
 
-  uint32_t t, wave, k_off, v_off;  // a lane's place in its wave's rows (ONE) or in its row
+  uint32_t t, wave, k_off, v_off;  // a lane's place in its wave's rows, or in its row
+  uint32_t step;                   // bytes from one step's rows to the next (kTiles)
 
   __device__ __forceinline__ Stage(const Args& a, uint32_t thread) : t(thread) {
     wave = THREADS == 64 ? 0 : uniform(thread >> 6);
     const uint32_t row = thread / kRowLanes, chunk = thread % kRowLanes;
     k_off = (WIDEN ? chunk : chunk ^ Swizzle::k(row)) * 16;
     v_off = (WIDEN ? chunk : chunk ^ Swizzle::v(row)) * 16;
-    if (ONE) {
+    if (kScalar) {
       k_off += row % kWaveRows * a.token_bytes;
       v_off += row % kWaveRows * a.token_bytes;
     }
+    step = kWaveRows * a.token_bytes;
   }
 
   __device__ __forceinline__ uint32_t row(int i) const {
-    return i * kRows + (ONE ? wave * kWaveRows : t / kRowLanes);
+    return i * kRows + (kScalar ? wave * kWaveRows : t / kRowLanes);
   }
 
   __device__ __forceinline__ void first(const Args& a, uint32_t pos, Rows& r) const {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kLooks; ++i) {
       split_pos(a, pos + row(i), &r.at[i], &r.token[i]);
-      if (ONE) {
+      if (kScalar) {
         r.at[i] = uniform(r.at[i]);
         r.token[i] = uniform(r.token[i]);
       }
@@ -239,7 +247,7 @@ struct Stage {
   __device__ __forceinline__ void next(const Args& a, uint32_t add_blocks, uint32_t add_tokens,
                                        Rows& r) const {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kLooks; ++i) {
       r.token[i] += add_tokens;
       const bool over = r.token[i] >= a.bs;
       r.token[i] = over ? r.token[i] - a.bs : r.token[i];
@@ -250,9 +258,9 @@ struct Stage {
   __device__ __forceinline__ void look(const Range& g, Rows& r) const {
     typedef const __attribute__((address_space(4))) uint32_t* scalar_list;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kLooks; ++i) {
       r.entry[i] = CLAIM_NONE;
-      if (ONE) {
+      if (kScalar) {
         // past the list: its last entry is read in its place
         const uint32_t at = r.at[i] < g.entries ? r.at[i] : g.entries - 1;
         const uint32_t entry = ((scalar_list)g.list)[at];
@@ -267,7 +275,7 @@ struct Stage {
     Places p;
     p.left = left;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kLooks; ++i) {
       p.entry[i] = r.entry[i] < a.nb ? r.entry[i] : CLAIM_NONE;
       p.byte[i] = (uint64_t)r.entry[i] * a.chunk_bytes + (uint64_t)r.token[i] * a.token_bytes;
     }
@@ -277,26 +285,31 @@ struct Stage {
   template <bool KEY>
   __device__ __forceinline__ void issue(const uint8_t* plane, const Places& p, uint8_t* tile,
                                         Held& held) const {
-    const uint32_t off = KEY ? k_off : v_off;
+    bool fine = p.left >= KEYS;  // every row is in the range and has a block
+#pragma unroll
+    for (int i = 0; i < kLooks; ++i) fine &= p.entry[i] != CLAIM_NONE;
+    const bool all = kScalar ? fine : __all(fine);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       if (WIDEN && KEYS < kRows && i * kRows + t / kRowLanes >= KEYS) break;
+      const int l = WITHIN == kTiles ? 0 : i;
       const uint32_t to = lds_address(tile) + i * THREADS * 16 + wave * 1024;
       // the first row of a step has a swizzle of its own where a step is less than 16 rows
-      const uint32_t mine = WIDEN ? off : off ^ (KEY ? Swizzle::k(i * kRows) : Swizzle::v(i * kRows)) * 16;
-      const uint8_t* base = ONE ? uniform(plane + p.byte[i]) : plane + p.byte[i];
-      const bool fine = p.entry[i] != CLAIM_NONE && row(i) + (ONE ? kWaveRows : 1) <= p.left;
-      if (ONE ? fine : __all(fine)) {
+      uint32_t off = KEY ? k_off : v_off;
+      if (!WIDEN) off ^= (KEY ? Swizzle::k(i * kRows) : Swizzle::v(i * kRows)) * 16;
+      if (WITHIN == kTiles) off += i * step;
+      const uint8_t* base = plane + p.byte[l];
+      if (all) {
         if constexpr (WIDEN)
-          held.r[i] = *(const u32x4*)(base + mine);
-        else if constexpr (ONE)
-          copy_to_lds(base, mine, to);
+          held.r[i] = *(const u32x4*)((kScalar ? uniform(base) : base) + off);
+        else if constexpr (kScalar)
+          copy_to_lds(uniform(base), off, to);
         else
-          copy_to_lds(base + mine, to);
+          copy_to_lds(base + off, to);
       } else {
         const bool there = i * kRows + t / kRowLanes < p.left;
-        const uint8_t* from = there && p.entry[i] != CLAIM_NONE
-                                  ? base + mine
+        const uint8_t* from = there && p.entry[l] != CLAIM_NONE
+                                  ? base + off
                                   : (const uint8_t*)kFill + (KEY && there ? 16 : 0);
         if constexpr (WIDEN)
           held.r[i] = *(const u32x4*)from;
@@ -784,10 +797,10 @@ __device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys
 // by every wave before any is in W(n), and is read first in M(n + 3), after a
 // barrier that every wave reaches with its copies done.
 
-template <int D, bool E4M3, int WAVES, bool ONE>
+template <int D, bool E4M3, int WAVES, Within WITHIN>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
   constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2, kAhead = 3;
-  using St = Stage<D * (E4M3 ? 1 : 2), E4M3, kKeys, WAVES * 64, ONE, WideSwizzle<D>>;
+  using St = Stage<D * (E4M3 ? 1 : 2), E4M3, kKeys, WAVES * 64, WITHIN, WideSwizzle<D>>;
   __shared__ __align__(1024) uint8_t lk[(kAhead + 1) * kTile];
   __shared__ __align__(1024) uint8_t lv[(kAhead + 1) * kTile];
   __shared__ uint32_t least[WAVES];
@@ -1168,12 +1181,12 @@ struct Few {
   };
 };
 
-template <int D, bool E4M3, bool ONE, int QT>
+template <int D, bool E4M3, Within WITHIN, int QT>
 __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
                                          typename Few<D, E4M3>::Lds& shared) {
   using F = Few<D, E4M3>;
   constexpr int M = 16 * QT, kKeys = F::kKeys, kTile = F::kTile, kWaves = F::kWaves;
-  using St = Stage<F::kBytes, false, kKeys, 64, ONE, NarrowSwizzle<F::kBytes>>;
+  using St = Stage<F::kBytes, false, kKeys, 64, WITHIN, NarrowSwizzle<F::kBytes>>;
   uint8_t* const lds = shared.ring;
   auto& tops = shared.tops;
   auto& sums = shared.sums;
@@ -1184,15 +1197,6 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
   const uint32_t split = b % splits, tile = b / splits;
   const Tile it = make_tile<M>(a, prefix, tile, split, splits, kv_head, kKeys);
   if (!it.any) return;
-  Row row[QT];
-  uint32_t least = ~0u;
-#pragma unroll
-  for (int c = 0; c < QT; ++c) {
-    row[c] = row_at(a, it, 16 * c + (t & 15));
-    uint32_t hi, lo;
-    seen_by_wave(row[c], 16, &hi, &lo);
-    least = lo < least ? lo : least;
-  }
   const uint64_t head_bytes = (uint64_t)kv_head * F::kBytes;
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
   // groups wave, wave + 4, ... of the range
@@ -1203,26 +1207,39 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
   uint8_t* const lv = lk + 2 * kTile;
   Narrow<D, E4M3, QT, kKeys> w;
   const St st(a, t);
-  if (pos < hi) {
-    const uint32_t add_blocks = kStep / a.bs, add_tokens = kStep % a.bs;
-    typename St::Rows rows, second;
-    typename St::Held none;
+  const uint32_t add_blocks = kStep / a.bs, add_tokens = kStep % a.bs;
+  const auto rest = [&](uint32_t from) { return from < hi ? hi - from : 0; };
+  typename St::Rows rows;
+  typename St::Places at;
+  typename St::Held none;
+  if (pos < hi) {  // copies begin before anything else
+    typename St::Rows second;
     st.first(a, pos, rows);
     second = rows;
     st.next(a, add_blocks, add_tokens, second);
     st.look(it.range, rows);
     st.look(it.range, second);
-    typename St::Places at = st.place(a, rows, hi - pos);
+    at = st.place(a, rows, hi - pos);
     st.template issue<true>(k, at, lk, none);
     st.template issue<false>(v, at, lv, none);
-    const auto rest = [&](uint32_t from) { return from < hi ? hi - from : 0; };
     at = st.place(a, second, rest(pos + kStep));
     st.template issue<true>(k, at, lk + kTile, none);
     st.template issue<false>(v, at, lv + kTile, none);
     rows = second;
     st.next(a, add_blocks, add_tokens, rows);
     st.look(it.range, rows);
-    w.start(a, row);
+  }
+  Row row[QT];
+  uint32_t least = ~0u;
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    row[c] = row_at(a, it, 16 * c + (t & 15));
+    uint32_t hi, lo;
+    seen_by_wave(row[c], 16, &hi, &lo);
+    least = lo < least ? lo : least;
+  }
+  w.start(a, row);
+  if (pos < hi) {
     uint32_t x = 0;
     constexpr int kLater = 3 * St::kSteps;  // copies begun after the one that is waited for
     const auto group = [&](auto masked) {
@@ -1253,8 +1270,6 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
 #pragma unroll 1
     for (; pos < hi; pos += kStep, x ^= kTile) group(std::true_type{});
     wait_loads();
-  } else {
-    w.start(a, row);
   }
   // join the waves: each row's common maximum first, then two and two
 #pragma unroll
@@ -1330,7 +1345,7 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
 // QT rows) in one launch, eight of the one kind and eight of the other in
 // turn: the first are bound by products and weights, the second by memory, and
 // two workgroups share a CU.
-template <int D, bool E4M3, bool ONE, int QT>
+template <int D, bool E4M3, Within WITHIN, int QT>
 __global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_items, uint32_t own_items) {
   __shared__ typename Few<D, E4M3>::Lds shared;
   const uint32_t b = blockIdx.x, of8 = b / 8;
@@ -1340,9 +1355,9 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_i
   const uint32_t item = (of8 < 2 * both ? of8 / 2 : of8 - both) * 8 + b % 8;
   if (item >= (prefix ? prefix_items : own_items)) return;
   if (prefix)
-    few_rows<D, E4M3, ONE, 2>(a, true, item, shared);
+    few_rows<D, E4M3, WITHIN, 2>(a, true, item, shared);
   else
-    few_rows<D, E4M3, ONE, QT>(a, false, item, shared);
+    few_rows<D, E4M3, WITHIN, QT>(a, false, item, shared);
 }
 
 // ------------------------------------------------------------------ joining
@@ -1468,31 +1483,42 @@ int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc
   return CLAIM_OK;
 }
 
-template <int D, bool E4M3, bool ONE>
-int launch_one(const PoolView& p, const Plan& plan, const Args& a) {
-  constexpr int kWaves = kRowsTile / 32;
-  const uint32_t own = plan.tiles * a.heads * a.own_splits;
-  const uint32_t prefix = plan.prefix_tiles * a.heads * a.prefix_splits;
-  const uint32_t narrow = plan.prefix_narrow ? prefix : 0;
-  const dim3 both((own + 7) / 8 * 8 + (narrow + 7) / 8 * 8), rows(kWaves * 64);
+template <int D, bool E4M3, Within WITHIN>
+void launch_few(const PoolView& p, const Plan& plan, const Args& a, uint32_t prefix, uint32_t own) {
+  const dim3 both((own + 7) / 8 * 8 + (prefix + 7) / 8 * 8);
   if (plan.columns == 1)
-    hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 1>), both, dim3(256), 0, p.stream, a, narrow, own);
-  else if (plan.columns == 2)
-    hipLaunchKernelGGL((k_attend_few<D, E4M3, ONE, 2>), both, dim3(256), 0, p.stream, a, narrow, own);
+    hipLaunchKernelGGL((k_attend_few<D, E4M3, WITHIN, 1>), both, dim3(256), 0, p.stream, a, prefix, own);
   else
-    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>), dim3(own), rows, 0, p.stream, a, 0u);
-  if (prefix > narrow)
-    hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, ONE>), dim3(prefix), rows, 0, p.stream, a, 1u);
-  if (plan.parts)
-    hipLaunchKernelGGL((k_join<D>), dim3((a.rows * a.heads * a.group + 3) / 4), dim3(256), 0, p.stream, a);
-  return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;
+    hipLaunchKernelGGL((k_attend_few<D, E4M3, WITHIN, 2>), both, dim3(256), 0, p.stream, a, prefix, own);
+}
+
+template <int D, bool E4M3, Within WITHIN>
+void launch_rows(const PoolView& p, const Args& a, uint32_t items, uint32_t prefix) {
+  constexpr int kWaves = kRowsTile / 32;
+  hipLaunchKernelGGL((k_attend_rows<D, E4M3, kWaves, WITHIN>), dim3(items), dim3(kWaves * 64), 0, p.stream,
+                     a, prefix);
 }
 
 template <int D, bool E4M3>
 int launch(const PoolView& p, const Plan& plan, const Args& a) {
-  // the rows of one load instruction in one block: see Stage
-  return p.bs % (64 * 16 / (D * (E4M3 ? 1 : 2))) == 0 ? launch_one<D, E4M3, true>(p, plan, a)
-                                                       : launch_one<D, E4M3, false>(p, plan, a);
+  const uint32_t own = plan.tiles * a.heads * a.own_splits;
+  const uint32_t prefix = plan.prefix_tiles * a.heads * a.prefix_splits;
+  const uint32_t narrow = plan.prefix_narrow ? prefix : 0;
+  const bool loads = p.bs % (1024 / (D * (E4M3 ? 1 : 2))) == 0;  // see Stage
+  if (plan.columns) {
+    if (p.bs % Few<D, E4M3>::kKeys == 0)
+      launch_few<D, E4M3, kTiles>(p, plan, a, narrow, own);
+    else if (loads)
+      launch_few<D, E4M3, kLoads>(p, plan, a, narrow, own);
+    else
+      launch_few<D, E4M3, kLanes>(p, plan, a, narrow, own);
+  }
+  const auto rows = loads ? launch_rows<D, E4M3, kLoads> : launch_rows<D, E4M3, kLanes>;
+  if (!plan.columns) rows(p, a, own, 0);
+  if (prefix > narrow) rows(p, a, prefix, 1);
+  if (plan.parts)
+    hipLaunchKernelGGL((k_join<D>), dim3((a.rows * a.heads * a.group + 3) / 4), dim3(256), 0, p.stream, a);
+  return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;
 }
 
 }  // namespace
