@@ -273,6 +273,7 @@ class Pool:
         self.kv = kv
         self.stream = stream
         self._stream_at, self._device_index = stream.cuda_stream, kv.device.index
+        self._current_stream = _current_stream()
         self.geometry = geometry
         self.seed = seed
         d = PoolDesc(
@@ -480,8 +481,9 @@ class Pool:
     def ordered(self, *tensors):
         """A with-block whose pool calls come after what the current stream
         has queued, and before what it queues next, also where the pool's
-        stream is another one; ``tensors`` are the arguments of those calls."""
-        if _current_stream(self._device_index) == self._stream_at:
+        stream is another one; ``tensors`` (or what has a record_stream) are
+        what those calls use."""
+        if self._current_stream(self._device_index) == self._stream_at:
             return _SAME_STREAM
         return _OtherStream(self.stream, tensors)
 
@@ -491,14 +493,13 @@ class Pool:
         return {name: getattr(t, name) for name, _ in CTiming._fields_}
 
 
-def _current_stream(device_index) -> int:
-    """The current stream's handle.  torch's own accessor of the handle is ten
-    times faster than making a Stream object to ask."""
+def _current_stream():
+    """A function of a device's index: the handle of its current stream.
+    torch's own accessor of the handle takes a tenth of the time that a Stream
+    object does."""
     torch = _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None:
-        return torch.cuda.current_stream(device_index).cuda_stream
-    return raw(device_index)
+    return getattr(torch._C, "_cuda_getCurrentRawStream",
+                   lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class _SameStream:

@@ -64,6 +64,7 @@ class Sequences:
         self._desc_at = ctypes.addressof(self._desc)
         self._device, self._bf16, self._int32 = dev, torch.bfloat16, torch.int32
         self._heads, self._dim = g.num_kv_heads, g.head_dim
+        self._lib = lib()
 
     # ------------------------------------------------------------- blocks
     def grow(self, ids, tokens):
@@ -71,36 +72,36 @@ class Sequences:
         (None: sequences 0..n-1), with blocks for them.  Returns the device
         tensor of statuses (SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED)."""
         at = 0 if ids is None else self._ints("ids", ids)
-        return self._entries(lib().claim_seqs_grow, "claim_seqs_grow", ids, at, "tokens", tokens)
+        return self._entries(self._lib.claim_seqs_grow, "claim_seqs_grow", ids, at, "tokens", tokens)
 
     def fork(self, parents, children):
         """claim_seqs_fork: the empty sequence ``children[i]`` becomes a copy
         of ``parents[i]`` that shares its full blocks.  Returns the statuses."""
         at = self._ints("parents", parents)
-        return self._entries(lib().claim_seqs_fork, "claim_seqs_fork", parents, at, "children", children)
+        return self._entries(self._lib.claim_seqs_fork, "claim_seqs_fork", parents, at, "children", children)
 
     def _entries(self, call, what, first, first_at, name, second):
         pool, second_at, n = self.pool, self._ints(name, second), second.numel()
         if first is not None and first.numel() != n:
             raise ValueError(f"{what} needs as many {name}")
         status = second.new_empty(n)
-        with pool.ordered(first, second, status, *self._state):
+        with pool.ordered(self, first, second, status):
             _check(call(pool._h, self._seqs_ref, first_at, second_at, n, status.data_ptr()), what)
         return status
 
     def free(self, ids) -> None:
         """claim_seqs_free: sequences ``ids`` give up their blocks."""
         pool, at = self.pool, self._ints("ids", ids)
-        with pool.ordered(ids, *self._state):
-            _check(lib().claim_seqs_free(pool._h, self._seqs_ref, at, ids.numel()), "claim_seqs_free")
+        with pool.ordered(self, ids):
+            _check(self._lib.claim_seqs_free(pool._h, self._seqs_ref, at, ids.numel()), "claim_seqs_free")
 
     def compact(self):
         """claim_seqs_compact: blocks in use move to the front of the pool.
         Returns the device tensor [1] of how many moved."""
         pool = self.pool
         moved = self.refs.new_empty(1)
-        with pool.ordered(moved, pool.kv, *self._state):
-            _check(lib().claim_seqs_compact(pool._h, self._seqs_ref, moved.data_ptr()),
+        with pool.ordered(self, moved):
+            _check(self._lib.claim_seqs_compact(pool._h, self._seqs_ref, moved.data_ptr()),
                    "claim_seqs_compact")
         return moved
 
@@ -117,8 +118,8 @@ class Sequences:
         _WRITE.pack_into(self._desc, 0, *self._kv(layer, rows, ids, offsets), k_scale, v_scale,
                          *self._rows("k", k, self._heads), *self._rows("v", v, self._heads))
         at = self._desc_at
-        with pool.ordered(k, v, ids, offsets, *self._state):
-            _check(lib().claim_kv_write(pool._h, self._seqs_ref, at, at + 40, at + 64),
+        with pool.ordered(self, k, v, ids, offsets):
+            _check(self._lib.claim_kv_write(pool._h, self._seqs_ref, at, at + 40, at + 64),
                    "claim_kv_write")
 
     def attend(self, layer: int, q, *, ids=None, offsets=None, scale: float | None = None,
@@ -142,36 +143,41 @@ class Sequences:
                             offsets, scale, k_scale, v_scale, out)
 
     def _attend(self, layer, q, prefix, prefix_at, blocks, ids, offsets, scale, k_scale, v_scale, out):
-        torch = _torch()
         pool, shape = self.pool, q.shape
         if len(shape) != 3:
             raise ValueError("q must be [rows, heads, head_dim]")
         heads = shape[1]
         rows_q = self._rows("q", q, heads)
         if out is None:
-            out = torch.empty(shape, dtype=self._bf16, device=self._device)
+            out = q.new_empty(shape)
         elif out.shape != shape:
             raise ValueError("out needs q's shape")
         given = (*self._kv(layer, shape[0], ids, offsets), k_scale, v_scale, *rows_q,
                  *self._rows("out", out, heads), heads, blocks, prefix_at,
                  self._dim**-0.5 if scale is None else scale, 0)
         _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
-        with pool.ordered(q, out, ids, offsets, prefix, pool.kv, *self._state):
-            rc = lib().claim_attend(pool._h, self._seqs_ref, self._desc_at)
+        with pool.ordered(self, q, out, ids, offsets, prefix):
+            rc = self._lib.claim_attend(pool._h, self._seqs_ref, self._desc_at)
             if rc == ENOSPC:  # the first call of a larger shape
                 need = ctypes.c_uint64()
-                _check(lib().claim_attend_work(pool._h, self._seqs_ref, self._desc_at,
+                _check(self._lib.claim_attend_work(pool._h, self._seqs_ref, self._desc_at,
                                                ctypes.byref(need)), "claim_attend_work")
                 # memory of the pool's stream: what was queued there may use
                 # the smaller one until it is done
+                torch = _torch()
                 with torch.cuda.stream(pool.stream):
                     self._work = torch.empty(need.value, dtype=torch.uint8, device=self._device)
                 self._work_at, self._work_bytes = self._work.data_ptr(), need.value
                 _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
-                rc = lib().claim_attend(pool._h, self._seqs_ref, self._desc_at)
+                rc = self._lib.claim_attend(pool._h, self._seqs_ref, self._desc_at)
             if rc != OK:
                 _check(rc, "claim_attend")
         return out
+
+    def record_stream(self, stream) -> None:
+        """The sequences' own tensors are used on ``stream``."""
+        for t in (*self._state, self.pool.kv):
+            t.record_stream(stream)
 
     # ------------------------------------------------------------ checks
     def _ints(self, name, t) -> int:
