@@ -519,7 +519,7 @@ const char* claim_strerror(int status);
  * identity it was registered with: claim_lookup does not hit it.  A claim
  * that recorded the block is judged as ever, by its own offload record. */
 typedef struct claim_seqs {
-  uint32_t max_seqs;   /* rows of tables */
+  uint32_t max_seqs;   /* rows of tables, at most 2^22 */
   uint32_t max_blocks; /* entries of a row */
   uint32_t* tables;    /* [max_seqs][max_blocks] */
   uint32_t* lengths;   /* [max_seqs] tokens */
@@ -587,7 +587,7 @@ typedef struct claim_rows {
 typedef struct claim_kv_desc {
   uint32_t layer;
   uint32_t num_seqs;
-  uint32_t num_rows;
+  uint32_t num_rows; /* at most 2^25 */
   uint32_t reserved; /* must be 0 */
   const uint32_t* ids;     /* [num_seqs] or NULL */
   const uint32_t* offsets; /* [num_seqs + 1], ascending from 0 to num_rows, or NULL */
@@ -618,7 +618,8 @@ int claim_kv_write(claim_pool* pool, const claim_seqs* seqs, const claim_kv_desc
  * read), once for all sequences.
  *
  * head_dim is 64 or 128, num_heads a multiple of num_kv_heads, at most 64
- * query heads to a KV head, else EINVAL.  work holds partial results:
+ * query heads to a KV head, num_rows x num_heads below 2^26 and num_seqs x
+ * num_kv_heads at most 2^22, else EINVAL.  out may be q.  work holds partial results:
  * claim_attend_work bytes (it goes by max_blocks and the counts alone, not
  * by lengths; it may be 0, work NULL), 256-byte aligned, used by this call
  * only, in stream order. */

@@ -1479,7 +1479,10 @@ int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc
   if (!finite_positive(d->scale)) return CLAIM_EINVAL;
   if ((uint64_t)d->prefix_blocks * p.bs > 0x7FFFFFFFull || (d->prefix_blocks && !d->prefix))
     return CLAIM_EINVAL;
-  if ((uint64_t)d->kv.num_rows * d->num_heads > 0x7FFFFFFFull) return CLAIM_EINVAL;
+  // a wave of the joining kernel for each row and query head, a workgroup of 512
+  // threads for each sequence and KV head: fewer than 2^32 threads
+  if ((uint64_t)d->kv.num_rows * d->num_heads >= 1u << 26 || (uint64_t)d->kv.num_seqs * p.heads > 1u << 22)
+    return CLAIM_EINVAL;
   return CLAIM_OK;
 }
 

@@ -20,11 +20,15 @@ struct PoolView {
 
 __attribute__((visibility("hidden"))) PoolView pool_view(const claim_pool* P);
 
-// Host-side checks shared by the sequence operators.
+// Host-side checks shared by the sequence operators.  The counts are limited so
+// that a launch of one workgroup a row, a sequence or a tile of theirs has fewer
+// than 2^32 threads.
+constexpr uint32_t kMostSeqs = 1u << 22, kMostRows = 1u << 25;
+
 inline int check_seqs(const claim_seqs* s) {
   if (!s || s->max_seqs == 0 || s->max_blocks == 0 || !s->tables || !s->lengths || !s->refs)
     return CLAIM_EINVAL;
-  if (s->max_seqs > (1u << 30) || (uint64_t)s->max_seqs * s->max_blocks > (1ull << 40))
+  if (s->max_seqs > kMostSeqs || (uint64_t)s->max_seqs * s->max_blocks > (1ull << 40))
     return CLAIM_EINVAL;
   return CLAIM_OK;
 }
@@ -36,7 +40,7 @@ inline bool scale_ok(float x) { return x >= 1e-30f && x <= 1e30f; }
 
 inline int check_kv(const PoolView& p, const claim_seqs* s, const claim_kv_desc* kv) {
   if (kv->reserved != 0 || p.planes_per_layer != 2 || kv->layer >= p.layers ||
-      (p.elem != 1 && p.elem != 2) || kv->num_seqs > s->max_seqs || kv->num_rows > 0x7FFFFFFFu)
+      (p.elem != 1 && p.elem != 2) || kv->num_seqs > s->max_seqs || kv->num_rows > kMostRows)
     return CLAIM_EINVAL;
   if (!kv->offsets && kv->num_rows != kv->num_seqs) return CLAIM_EINVAL;
   if (kv->num_rows > 0 && kv->num_seqs == 0) return CLAIM_EINVAL;

@@ -247,3 +247,16 @@ def test_blocks_past_32_bits(torch, ck):
     want = torch.einsum("hij,jhd->ihd", p, data[1].double())
     size = torch.einsum("hij,jhd->ihd", p, data[1].double().abs())
     assert ((out - want).abs() <= 1.01 * (2.0**-8 * want.abs() + (2.0**-8 + 2.0**-14) * size)).all()
+
+
+@pytest.mark.parametrize("seqs, prefix_blocks", [([(300, 40), (7, 0)], 0), ([(1, 900)], 0), ([(1, 30)] * 5, 20)],
+                         ids=["rows", "split", "shared"])
+def test_out_may_be_q(torch, ck, seqs, prefix_blocks):
+    w = World(torch, seqs=seqs, heads=2, group=4, dim=64, prefix_blocks=prefix_blocks, seed=18)
+    pool, s, d = w.to_gpu(ck)
+    with pool:
+        if prefix_blocks:
+            got = s.attend_shared(w.layer, d.q, d.prefix, offsets=d.offsets, out=d.q)
+        else:
+            got = s.attend(w.layer, d.q, offsets=d.offsets, out=d.q)
+        check(got, *w.expected())

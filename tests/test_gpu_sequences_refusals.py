@@ -190,3 +190,23 @@ def test_nothing_to_do(torch, ck):
         off = torch.zeros(4, dtype=torch.int32, device="cuda")
         assert seqs.attend(0, q, offsets=off).shape == (0, 4, 64)
         assert not kv.any()
+
+
+@pytest.mark.parametrize("change, seqs_change", [
+    ({"kv.num_rows": 2**25 + 1, "kv.offsets": 256}, {}),  # refused before anything is read
+    ({"kv.num_rows": 2**31, "kv.offsets": 256}, {}),
+    ({}, {"max_seqs": 2**22 + 1})], ids=str)
+def test_counts_past_the_limits(torch, ck, change, seqs_change):
+    pool, seqs, _ = world(torch, ck)
+    with pool:
+        assert call(ck, seqs, "attend", change, seqs_change) == ck.EINVAL
+        assert call(ck, seqs, "write", change, seqs_change) == ck.EINVAL
+
+
+@pytest.mark.parametrize("change, seqs_change", [
+    ({"kv.num_rows": 2**24, "kv.offsets": 256}, {}),  # of 4 heads: 2^26 rows and heads
+    ({"kv.num_seqs": 2**21 + 1, "kv.offsets": 256}, {"max_seqs": 2**22})], ids=str)  # of 2 KV heads
+def test_attention_past_the_limits(torch, ck, change, seqs_change):
+    pool, seqs, _ = world(torch, ck)
+    with pool:
+        assert call(ck, seqs, "attend", change, seqs_change) == ck.EINVAL
