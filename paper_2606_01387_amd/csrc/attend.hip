@@ -1459,7 +1459,12 @@ Plan make_plan(const PoolView& p, const claim_seqs* s, const claim_attend_desc* 
     r.prefix_narrow = r.columns && rows * d->num_heads * prefix <= (8u << 20);
     const uint32_t tile = r.prefix_narrow ? kPrefixTile : kRowsTile;
     r.prefix_tiles = (uint32_t)((rows * group + tile - 1) / tile);
-    r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, (r.prefix_narrow ? 2ull : 1ull) * p.cus, prefix, 256);
+    // k_attend_rows is slow to begin (its first tiles, then 256 rows of parts to
+    // store): half of the CUs with 512 keys each take the time that all take with
+    // 256, and leave half the parts to join.  64 sequences of 1024 own tokens
+    // behind 8192: 74.8 us with splits from 256 keys on, 70.1 from 512, 76.7 from 1024.
+    r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, (r.prefix_narrow ? 2ull : 1ull) * p.cus, prefix,
+                                 r.prefix_narrow ? 256 : 512);
   }
   const uint64_t splits = (uint64_t)r.own_splits + r.prefix_splits;
   r.parts = splits > 1 ? rows * d->num_heads * splits : 0;
