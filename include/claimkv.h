@@ -511,9 +511,10 @@ const char* claim_strerror(int status);
  * Sequence r has lengths[r] tokens; position p of it lies in block
  * tables[r * max_blocks + p / block_size], at token p % block_size of the
  * block; entries past its last block are CLAIM_NONE.  refs[b] counts the
- * table entries that name block b: a block with refs 0 is free.  A program
- * starts with tables all CLAIM_NONE, lengths and refs 0, and may hold blocks
- * of its own (a claim's, until it is restored) by a count in refs.
+ * table entries that name block b, at most 2^31 - 1: a block with refs 0 is
+ * free.  A program starts with tables all CLAIM_NONE, lengths and refs 0, and
+ * may hold blocks of its own (a claim's, until it is restored) by a count in
+ * refs.
  *
  * A block handed out (by grow, fork, compact) no longer holds the cache
  * identity it was registered with: claim_lookup does not hit it.  A claim
