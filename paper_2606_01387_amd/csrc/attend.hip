@@ -641,7 +641,56 @@ __device__ __forceinline__ uint32_t find_tile(const Args& a, uint32_t tile) {
   return uniform(lo);
 }
 
+// The item `place` where tiles of longer sequences come before those of shorter
+// ones, and a sequence's late tiles, which see the most, before its early ones:
+// a workgroup that starts late has little left to do.  A lane holds a sequence
+// and counts the tiles of those before it.  Ragged prompts of up to 1500 tokens
+// behind up to 4000, 28 query heads over 4 of 128: 8 of them 302 us so and 320 us
+// in the order they come in, 12 of them in e4m3 331 and 342 us.
+constexpr uint32_t kOrdered = 64;  // sequences at most
+
+struct Ordered {
+  bool any;
+  uint32_t part, first, n, id, len;
+};
+
 template <int M>
+__device__ __forceinline__ Ordered ordered_tile(const Args& a, uint32_t place) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t first = 0, n = 0, id = 0, len = 0;
+  if (lane < a.num_seqs) {
+    first = a.offsets[lane];
+    n = a.offsets[lane + 1] - first;
+    id = a.ids ? a.ids[lane] : lane;
+    // offsets that run backwards or past the rows give the sequence none
+    if (first > a.rows || n > a.rows - first) n = 0;
+    if (id < a.max_seqs) len = a.lengths[id];
+  }
+  const uint32_t mine = (n * a.group + M - 1) / M;
+  // one number decides: the length (beyond 2^26 all are alike), then the lane
+  const uint32_t key = (len < 1u << 26 ? len : (1u << 26) - 1) << 6 | (63 - lane);
+  uint32_t before = 0;
+  for (uint32_t s0 = 0; s0 < a.num_seqs; s0 += 8) {
+#pragma unroll
+    for (uint32_t s = s0; s < s0 + 8; ++s) {  // lanes without a sequence have no tiles
+      const uint32_t tiles = __builtin_amdgcn_readlane(mine, s);
+      before += (uint32_t)__builtin_amdgcn_readlane(key, s) > key ? tiles : 0;
+    }
+  }
+  const uint64_t m = __ballot(place - before < mine);
+  const uint32_t s = m ? (uint32_t)__builtin_ctzll(m) : 0;
+  Ordered r;
+  r.any = m != 0;
+  r.part = __builtin_amdgcn_readlane(before + mine, s) - 1 - place;
+  r.first = __builtin_amdgcn_readlane(first, s);
+  r.n = __builtin_amdgcn_readlane(n, s);
+  r.id = __builtin_amdgcn_readlane(id, s);
+  r.len = __builtin_amdgcn_readlane(len, s);
+  return r;
+}
+
+// ORDERED: `tile` is a place in the order above where there is one.
+template <int M, bool ORDERED>
 __device__ __forceinline__ Tile make_tile(const Args& a, bool prefix, uint32_t tile, uint32_t split,
                                           uint32_t splits, uint32_t kv_head, uint32_t align) {
   Tile it;
@@ -659,32 +708,44 @@ __device__ __forceinline__ Tile make_tile(const Args& a, bool prefix, uint32_t t
     it.range.entries = a.prefix_tokens / a.bs;
     top = a.prefix_tokens;
   } else {
-    uint32_t s, part;
-    if (a.offsets) {
-      s = find_tile<M>(a, tile);
-      const uint32_t from = a.offsets[s], start = first_tile<M>(a, s);
-      it.first = from;
-      it.n = a.offsets[s + 1] - from;
-      part = tile - start;
-      // offsets that run backwards or past the rows give the sequence none
-      it.any = tile >= start && from <= a.rows && it.n <= a.rows - from;
+    uint32_t part, id, len;
+    if (ORDERED && a.offsets && a.num_seqs <= kOrdered) {
+      const Ordered r = ordered_tile<M>(a, tile);
+      it.any = r.any;
+      it.first = r.first;
+      it.n = r.n;
+      part = r.part;
+      id = r.id;
+      len = r.len;
     } else {
-      const uint32_t per = (a.group + M - 1) / M;
-      s = per == 1 ? tile : tile / per;
-      part = tile - s * per;
-      it.first = s;
-      it.n = 1;
-      it.any = s < a.num_seqs;
-      if (!it.any) s = 0;
+      if (ORDERED) tile = a.tiles - 1 - tile;  // late rows first
+      uint32_t s;
+      if (a.offsets) {
+        s = find_tile<M>(a, tile);
+        const uint32_t from = a.offsets[s], start = first_tile<M>(a, s);
+        it.first = from;
+        it.n = a.offsets[s + 1] - from;
+        part = tile - start;
+        // offsets that run backwards or past the rows give the sequence none
+        it.any = tile >= start && from <= a.rows && it.n <= a.rows - from;
+      } else {
+        const uint32_t per = (a.group + M - 1) / M;
+        s = per == 1 ? tile : tile / per;
+        part = tile - s * per;
+        it.first = s;
+        it.n = 1;
+        it.any = s < a.num_seqs;
+        if (!it.any) s = 0;
+      }
+      id = a.ids ? a.ids[s] : s;
+      len = id < a.max_seqs ? a.lengths[id] : 0;
     }
     it.all = it.any ? it.n * a.group : 0;
     it.any = it.any && part <= it.all / M;
     it.x0 = it.any ? part * M : 0;
     it.any = it.any && it.x0 < it.all;
-    const uint32_t id = a.ids ? a.ids[s] : s;
-    const bool fine = id < a.max_seqs;
-    it.len = fine ? a.lengths[id] : 0;
-    it.range.list = a.tables + (uint64_t)(fine ? id : 0) * a.max_blocks;
+    it.len = len;
+    it.range.list = a.tables + (uint64_t)(id < a.max_seqs ? id : 0) * a.max_blocks;
     it.range.entries = a.max_blocks;
     lo = a.prefix_tokens;
     const uint32_t last = it.x0 + M < it.all ? it.x0 + M : it.all;
@@ -809,9 +870,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   const uint32_t kv_head = b % a.heads;  // one head's keys stay in one die's cache where heads = 8
   b /= a.heads;
   const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
-  const uint32_t split = b % splits, tiles = prefix ? a.prefix_tiles : a.tiles;
-  const uint32_t tile = tiles - 1 - b / splits;  // late rows see the most: they start first
-  const Tile it = make_tile<M>(a, prefix, tile, split, splits, kv_head, kKeys);
+  const uint32_t split = b % splits;
+  const Tile it = make_tile<M, true>(a, prefix, b / splits, split, splits, kv_head, kKeys);
   if (!it.any) return;
   const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
@@ -1195,7 +1255,7 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
   b /= a.heads;
   const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
   const uint32_t split = b % splits, tile = b / splits;
-  const Tile it = make_tile<M>(a, prefix, tile, split, splits, kv_head, kKeys);
+  const Tile it = make_tile<M, false>(a, prefix, tile, split, splits, kv_head, kKeys);
   if (!it.any) return;
   const uint64_t head_bytes = (uint64_t)kv_head * F::kBytes;
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;

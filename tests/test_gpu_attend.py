@@ -260,3 +260,17 @@ def test_out_may_be_q(torch, ck, seqs, prefix_blocks):
         else:
             got = s.attend(w.layer, d.q, offsets=d.offsets, out=d.q)
         check(got, *w.expected())
+
+
+def test_more_prompts_than_lanes(torch, ck):
+    """Enough sequences that their order is not one of a wave's lanes."""
+    seqs = [(17 + s % 9, s % 40) for s in range(68)] + [(0, 5), (33, 0)]
+    w = World(torch, seqs=seqs, heads=1, group=8, dim=64, seed=19)
+    check(attend(ck, w), *w.expected())
+
+
+def test_prompts_of_equal_and_of_no_length(torch, ck):
+    """Sequences in the order of their lengths: some alike, some with nothing."""
+    seqs = [(40, 10), (0, 0), (50, 0), (40, 10), (0, 50), (33, 17), (90, 0), (1, 0)]
+    w = World(torch, seqs=seqs, heads=2, group=8, dim=64, seed=20)
+    check(attend(ck, w), *w.expected())
