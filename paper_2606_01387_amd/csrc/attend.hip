@@ -858,15 +858,25 @@ __device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys
 // by every wave before any is in W(n), and is read first in M(n + 3), after a
 // barrier that every wave reaches with its copies done.
 
+template <int D, int WAVES>
+struct Many {
+  static constexpr int kKeys = 64, kTile = kKeys * D * 2, kAhead = 3;
+  struct Lds {
+    __align__(1024) uint8_t k[(kAhead + 1) * kTile];
+    __align__(1024) uint8_t v[(kAhead + 1) * kTile];
+    uint32_t least[WAVES];
+  };
+};
+
 template <int D, bool E4M3, int WAVES, Within WITHIN>
-__global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
-  constexpr int M = WAVES * 32, kKeys = 64, kTile = kKeys * D * 2, kAhead = 3;
+__device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b,
+                                          typename Many<D, WAVES>::Lds& shared) {
+  using F = Many<D, WAVES>;
+  constexpr int M = WAVES * 32, kKeys = F::kKeys, kTile = F::kTile, kAhead = F::kAhead;
   using St = Stage<D * (E4M3 ? 1 : 2), E4M3, kKeys, WAVES * 64, WITHIN, WideSwizzle<D>>;
-  __shared__ __align__(1024) uint8_t lk[(kAhead + 1) * kTile];
-  __shared__ __align__(1024) uint8_t lv[(kAhead + 1) * kTile];
-  __shared__ uint32_t least[WAVES];
+  uint8_t *const lk = shared.k, *const lv = shared.v;
+  auto& least = shared.least;
   const uint32_t t = threadIdx.x;
-  uint32_t b = blockIdx.x;
   const uint32_t kv_head = b % a.heads;  // one head's keys stay in one die's cache where heads = 8
   b /= a.heads;
   const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
@@ -993,6 +1003,12 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
   } else {
     w.finish(a, row);
   }
+}
+
+template <int D, bool E4M3, int WAVES, Within WITHIN>
+__global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t prefix) {
+  __shared__ typename Many<D, WAVES>::Lds shared;
+  many_rows<D, E4M3, WAVES, WITHIN>(a, prefix, blockIdx.x, shared);
 }
 
 // ------------------------------------------------------------ few query rows
@@ -1228,9 +1244,9 @@ struct Narrow {
   }
 };
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, int WAVES>
 struct Few {
-  static constexpr int kWaves = 4, kBytes = D * (E4M3 ? 1 : 2);
+  static constexpr int kWaves = WAVES, kBytes = D * (E4M3 ? 1 : 2);
   static constexpr int kKeys = kBytes == 256 ? 16 : 32;  // LDS for two workgroups on a CU
   static constexpr int kTile = kKeys * kBytes;
   static constexpr int kRing = kWaves * 4 * kTile;
@@ -1241,10 +1257,10 @@ struct Few {
   };
 };
 
-template <int D, bool E4M3, Within WITHIN, int QT>
+template <int D, bool E4M3, int WAVES, Within WITHIN, int QT>
 __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
-                                         typename Few<D, E4M3>::Lds& shared) {
-  using F = Few<D, E4M3>;
+                                         typename Few<D, E4M3, WAVES>::Lds& shared) {
+  using F = Few<D, E4M3, WAVES>;
   constexpr int M = 16 * QT, kKeys = F::kKeys, kTile = F::kTile, kWaves = F::kWaves;
   using St = Stage<F::kBytes, false, kKeys, 64, WITHIN, NarrowSwizzle<F::kBytes>>;
   uint8_t* const lds = shared.ring;
@@ -1351,7 +1367,7 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
     for (int j = 0; j < D / 16; ++j) w.o[c][j] *= f;
   }
   constexpr uint32_t kPart = M * D;  // floats of one wave
-  static_assert(kPart * 4 * 2 <= F::kRing, "two waves' parts fit");
+  static_assert(kPart * 4 * kWaves / 2 <= F::kRing, "two waves' parts fit");
   float* const parts = (float*)lds;
 #pragma unroll
   for (uint32_t half = kWaves / 2; half > 0; half /= 2) {
@@ -1407,7 +1423,7 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
 // two workgroups share a CU.
 template <int D, bool E4M3, Within WITHIN, int QT>
 __global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_items, uint32_t own_items) {
-  __shared__ typename Few<D, E4M3>::Lds shared;
+  __shared__ typename Few<D, E4M3, 4>::Lds shared;
   const uint32_t b = blockIdx.x, of8 = b / 8;
   const uint32_t prefix8 = (prefix_items + 7) / 8, own8 = (own_items + 7) / 8;
   const uint32_t both = prefix8 < own8 ? prefix8 : own8;
@@ -1415,9 +1431,28 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_i
   const uint32_t item = (of8 < 2 * both ? of8 / 2 : of8 - both) * 8 + b % 8;
   if (item >= (prefix ? prefix_items : own_items)) return;
   if (prefix)
-    few_rows<D, E4M3, WITHIN, 2>(a, true, item, shared);
+    few_rows<D, E4M3, 4, WITHIN, 2>(a, true, item, shared);
   else
-    few_rows<D, E4M3, WITHIN, QT>(a, false, item, shared);
+    few_rows<D, E4M3, 4, WITHIN, QT>(a, false, item, shared);
+}
+
+// Items of a long prefix by many_rows, then items of the sequences' own keys by
+// few_rows with eight waves, in one launch: the first keep the matrix cores of
+// some CUs busy and little memory, the second memory, and CUs that are done with
+// the one kind take up the other.  64 sequences of up to 1024 own tokens behind
+// 8192, 8 KV heads of 128 for 4 query heads each: 57 us with the join, where
+// the two kinds one after another take 41 and 27 us.
+template <int D, bool E4M3, Within WITHIN>
+__global__ void __launch_bounds__(512, 2) k_attend_both(Args a, uint32_t prefix_items) {
+  __shared__ union {
+    typename Many<D, 8>::Lds many;
+    typename Few<D, E4M3, 8>::Lds few;
+  } shared;
+  const uint32_t b = blockIdx.x;
+  if (b < prefix_items)
+    many_rows<D, E4M3, 8, kLoads>(a, true, b, shared.many);
+  else
+    few_rows<D, E4M3, 8, WITHIN, 1>(a, false, b - prefix_items, shared.few);
 }
 
 // ------------------------------------------------------------------ joining
@@ -1483,8 +1518,9 @@ __global__ void __launch_bounds__(256) k_join(Args a) {
 // --------------------------------------------------------------------- host
 
 struct Plan {
-  uint32_t columns;  // own keys by k_attend_few with 16 x columns rows a tile; 0: by k_attend_rows
-  bool prefix_narrow;  // the prefix in k_attend_few's launch, else by k_attend_rows
+  uint32_t columns;    // own keys by few_rows with 16 x columns rows a tile; 0: by many_rows
+  bool prefix_narrow;  // the prefix by few_rows, in k_attend_few's launch; else by many_rows
+  bool both;           // ... in k_attend_both's launch, with the own keys
   uint32_t own_splits, prefix_splits, tiles, prefix_tiles;
   uint64_t parts;  // parts of all rows and heads; 0: none are kept
 };
@@ -1499,6 +1535,9 @@ uint32_t splits_for(uint64_t groups, uint64_t slots, uint64_t keys, uint64_t lea
   return (uint32_t)(got < 1 ? 1 : got > kMostSplits ? kMostSplits : got);
 }
 
+// Whether the rows of one load instruction of a wave lie in one block (see Stage).
+bool one_block_loads(const PoolView& p) { return p.bs % (1024 / (p.dim * p.elem)) == 0; }
+
 Plan make_plan(const PoolView& p, const claim_seqs* s, const claim_attend_desc* d) {
   Plan r{};
   const uint64_t group = d->num_heads / p.heads, rows = d->kv.num_rows, seqs = d->kv.num_seqs;
@@ -1509,23 +1548,34 @@ Plan make_plan(const PoolView& p, const claim_seqs* s, const claim_attend_desc* 
   r.columns = each <= 16 ? 1 : each <= 64 ? 2 : 0;
   const uint32_t M = r.columns ? 16 * r.columns : kRowsTile;
   r.tiles = (uint32_t)(d->kv.offsets ? rows * group / M + seqs : seqs * ((group + M - 1) / M));
-  r.own_splits = splits_for((uint64_t)r.tiles * p.heads, r.columns ? 2ull * p.cus : p.cus, own,
-                            r.columns ? 256 : 512);
+  const uint64_t groups = (uint64_t)r.tiles * p.heads;
   if (prefix) {
-    // few_rows makes 0.3 M (query row, key) pairs a microsecond beside the own
-    // keys and in their launch; k_attend_rows makes 2.4 M after 14 us, in a launch
-    // of its own.  8192 shared tokens, 8 KV heads, 4 query heads each, 4 / 16 / 64
-    // sequences: 22 / 32 / 65 us and 31 / 32 / 40 us.
-    r.prefix_narrow = r.columns && rows * d->num_heads * prefix <= (8u << 20);
-    const uint32_t tile = r.prefix_narrow ? kPrefixTile : kRowsTile;
-    r.prefix_tiles = (uint32_t)((rows * group + tile - 1) / tile);
-    // k_attend_rows is slow to begin (its first tiles, then 256 rows of parts to
+    // The wide tile is slow to begin (its first keys, then 256 rows of parts to
     // store): half of the CUs with 512 keys each take the time that all take with
-    // 256, and leave half the parts to join.  64 sequences of 1024 own tokens
-    // behind 8192: 74.8 us with splits from 256 keys on, 70.1 from 512, 76.7 from 1024.
-    r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, (r.prefix_narrow ? 2ull : 1ull) * p.cus, prefix,
-                                 r.prefix_narrow ? 256 : 512);
+    // 256, and leave half the parts to join.  64 sequences of up to 1024 own tokens
+    // behind 8192, 8 KV heads of 128 for 4 query heads each: 74.8 us with splits
+    // from 256 keys on, 70.1 from 512, 76.7 from 1024 (in launches of their own).
+    r.prefix_tiles = (uint32_t)((rows * group + kRowsTile - 1) / kRowsTile);
+    r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, p.cus, prefix, 512);
+    // One launch for both kinds of keys where a CU has two items of own keys at
+    // most, as they have a CU to themselves there: the same 70.4 -> 64.2 us, but 256
+    // sequences with nothing of their own 75 -> 94 us.
+    r.both = r.columns == 1 && one_block_loads(p) && groups <= 2ull * p.cus;
+    // Narrow tiles make 0.2 to 0.3 M (query row, key) pairs a microsecond, all CUs
+    // together; a wide one, full or not, 32 keys, and 10 us more where it needs a
+    // launch of its own.  8192 shared tokens, 8 KV heads for 4 query heads each, 8 /
+    // 16 / 32 sequences: 21.6 / 30.2 / 37.7 us narrow and 25.6 / 25.6 / 27.2 us wide;
+    // 30000 tokens, one KV head for 8, 12 sequences: 23.1 and 29.9 us.
+    const uint64_t wide = 6144 * (prefix / r.prefix_splits) + (r.both ? 0 : 3u << 20);
+    r.prefix_narrow = r.columns && rows * d->num_heads * prefix <= wide;
+    if (r.prefix_narrow) {
+      r.both = false;
+      r.prefix_tiles = (uint32_t)((rows * group + kPrefixTile - 1) / kPrefixTile);
+      r.prefix_splits = splits_for((uint64_t)r.prefix_tiles * p.heads, 2ull * p.cus, prefix, 256);
+    }
   }
+  // k_attend_few's workgroups run two to a CU
+  r.own_splits = splits_for(groups, r.columns && !r.both ? 2ull * p.cus : p.cus, own, r.columns ? 256 : 512);
   const uint64_t splits = (uint64_t)r.own_splits + r.prefix_splits;
   r.parts = splits > 1 ? rows * d->num_heads * splits : 0;
   return r;
@@ -1572,9 +1622,14 @@ int launch(const PoolView& p, const Plan& plan, const Args& a) {
   const uint32_t own = plan.tiles * a.heads * a.own_splits;
   const uint32_t prefix = plan.prefix_tiles * a.heads * a.prefix_splits;
   const uint32_t narrow = plan.prefix_narrow ? prefix : 0;
-  const bool loads = p.bs % (1024 / (D * (E4M3 ? 1 : 2))) == 0;  // see Stage
-  if (plan.columns) {
-    if (p.bs % Few<D, E4M3>::kKeys == 0)
+  const bool loads = one_block_loads(p);
+  if (plan.both) {
+    if (p.bs % Few<D, E4M3, 8>::kKeys == 0)
+      hipLaunchKernelGGL((k_attend_both<D, E4M3, kTiles>), dim3(prefix + own), dim3(512), 0, p.stream, a, prefix);
+    else
+      hipLaunchKernelGGL((k_attend_both<D, E4M3, kLoads>), dim3(prefix + own), dim3(512), 0, p.stream, a, prefix);
+  } else if (plan.columns) {
+    if (p.bs % Few<D, E4M3, 4>::kKeys == 0)
       launch_few<D, E4M3, kTiles>(p, plan, a, narrow, own);
     else if (loads)
       launch_few<D, E4M3, kLoads>(p, plan, a, narrow, own);
@@ -1583,7 +1638,7 @@ int launch(const PoolView& p, const Plan& plan, const Args& a) {
   }
   const auto rows = loads ? launch_rows<D, E4M3, kLoads> : launch_rows<D, E4M3, kLanes>;
   if (!plan.columns) rows(p, a, own, 0);
-  if (prefix > narrow) rows(p, a, prefix, 1);
+  if (prefix > narrow && !plan.both) rows(p, a, prefix, 1);
   if (plan.parts)
     hipLaunchKernelGGL((k_join<D>), dim3((a.rows * a.heads * a.group + 3) / 4), dim3(256), 0, p.stream, a);
   return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;

@@ -274,3 +274,15 @@ def test_prompts_of_equal_and_of_no_length(torch, ck):
     seqs = [(40, 10), (0, 0), (50, 0), (40, 10), (0, 50), (33, 17), (90, 0), (1, 0)]
     w = World(torch, seqs=seqs, heads=2, group=8, dim=64, seed=20)
     check(attend(ck, w), *w.expected())
+
+
+# 5600 shared keys of 640 query rows and heads are worth a wide tile of rows in the
+# launch of the own keys, of 1280 one in a launch of its own
+@pytest.mark.parametrize("block_size, dim, e4m3, group, times", [
+    (16, 128, False, 16, 5), (16, 128, True, 16, 5), (8, 64, False, 16, 5), (64, 64, True, 16, 5),
+    (5, 128, False, 16, 10), (16, 64, False, 32, 5)])
+def test_a_long_prefix_of_many_rows(torch, ck, block_size, dim, e4m3, group, times):
+    seqs = [(1, m) for m in (0, 1, 15, 40, 333, 0, 64, 7) * times]
+    w = World(torch, seqs=seqs, heads=1, group=group, dim=dim, block_size=block_size, e4m3=e4m3,
+              prefix_blocks=5600 // block_size, seed=21)
+    check(attend(ck, w, prefix=True), *w.expected())
