@@ -38,6 +38,12 @@
  *                  that cannot allocate (graph capture, serving loops);
  *   claim_digest_grid     the digest grid a launch takes.
  *
+ * A serving program keeps its running sequences on the same blocks with the
+ * calls at the end of this file: claim_seqs_grow, claim_seqs_fork,
+ * claim_seqs_free and claim_seqs_compact hand blocks out, share, take back and
+ * move them, claim_blocks_copy copies them, claim_kv_write fills them and
+ * claim_attend reads them.
+ *
  * The digest, keys and chain are this library's definitions (the paper
  * leaves the byte-level check open; section 7 path B only requires
  * affected-block evidence for the failure):
@@ -133,7 +139,8 @@ typedef struct claim_pool claim_pool;
  * planes_per_layer = 2, p = layer for an MLA latent (planes_per_layer = 1);
  * a chunk is block_size x num_kv_heads x head_dim elements of elem_bytes
  * bytes in [token][head][dim] order, and must be a multiple of 16 bytes.
- * Element bytes are never interpreted (bf16 and fp8 are hashed as bytes).
+ * Claims never interpret element bytes (bf16 and fp8 are hashed as bytes);
+ * claim_kv_write and claim_attend do.
  *
  * A pool may hold a head shard of every block, as one GPU does under tensor
  * parallelism by KV head: heads [first_kv_head, first_kv_head +

