@@ -1449,23 +1449,27 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_i
     few_rows<D, E4M3, 4, WITHIN, QT>(a, false, item, shared);
 }
 
-// Items of a long prefix by many_rows, then items of the sequences' own keys by
+// Items of a long prefix by many_rows and items of the sequences' own keys by
 // few_rows with eight waves, in one launch: the first keep the matrix cores of
 // some CUs busy and little memory, the second memory, and CUs that are done with
-// the one kind take up the other.  64 sequences of up to 1024 own tokens behind
+// the one kind take up the other.  The prefix's items, which are the longer ones,
+// begin where they leave a quarter of the CUs to the others, else they come last:
+// 128 of them and 512 of nothing 32 us first and 41 us last, 252 and 200 of up to
+// 2000 e4m3 tokens 55 us first and 51 us last.  64 sequences of up to 1024 own tokens behind
 // 8192, 8 KV heads of 128 for 4 query heads each: 57 us with the join, where
 // the two kinds one after another take 41 and 27 us.
 template <int D, bool E4M3, Within WITHIN>
-__global__ void __launch_bounds__(512, 2) k_attend_both(Args a, uint32_t prefix_items) {
+__global__ void __launch_bounds__(512, 2) k_attend_both(Args a, uint32_t prefix_items, bool prefix_first) {
   __shared__ union {
     typename Many<D, 8>::Lds many;
     typename Few<D, E4M3, 8>::Lds few;
   } shared;
-  const uint32_t b = blockIdx.x;
-  if (b < prefix_items)
-    many_rows<D, E4M3, 8, kLoads>(a, true, b, shared.many);
+  const uint32_t b = blockIdx.x, own_items = gridDim.x - prefix_items;
+  const uint32_t prefix_from = prefix_first ? 0 : own_items, own_from = prefix_first ? prefix_items : 0;
+  if (prefix_first ? b < prefix_items : b >= own_items)
+    many_rows<D, E4M3, 8, kLoads>(a, true, b - prefix_from, shared.many);
   else
-    few_rows<D, E4M3, 8, WITHIN, 1>(a, false, b - prefix_items, shared.few);
+    few_rows<D, E4M3, 8, WITHIN, 1>(a, false, b - own_from, shared.few);
 }
 
 // ------------------------------------------------------------------ joining
@@ -1639,10 +1643,13 @@ int launch(const PoolView& p, const Plan& plan, const Args& a) {
   const uint32_t narrow = plan.prefix_narrow ? prefix : 0;
   const bool loads = one_block_loads(p);
   if (plan.both) {
+    const bool first = 4 * prefix <= 3 * p.cus;
     if (p.bs % Few<D, E4M3, 8>::kKeys == 0)
-      hipLaunchKernelGGL((k_attend_both<D, E4M3, kTiles>), dim3(prefix + own), dim3(512), 0, p.stream, a, prefix);
+      hipLaunchKernelGGL((k_attend_both<D, E4M3, kTiles>), dim3(prefix + own), dim3(512), 0, p.stream, a, prefix,
+                         first);
     else
-      hipLaunchKernelGGL((k_attend_both<D, E4M3, kLoads>), dim3(prefix + own), dim3(512), 0, p.stream, a, prefix);
+      hipLaunchKernelGGL((k_attend_both<D, E4M3, kLoads>), dim3(prefix + own), dim3(512), 0, p.stream, a, prefix,
+                         first);
   } else if (plan.columns) {
     if (p.bs % Few<D, E4M3, 4>::kKeys == 0)
       launch_few<D, E4M3, kTiles>(p, plan, a, narrow, own);
