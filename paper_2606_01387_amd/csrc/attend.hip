@@ -1456,8 +1456,8 @@ __global__ void __launch_bounds__(256, 2) k_attend_few(Args a, uint32_t prefix_i
 // begin where they leave a quarter of the CUs to the others, else they come last:
 // 128 of them and 512 of nothing 32 us first and 41 us last, 252 and 200 of up to
 // 2000 e4m3 tokens 55 us first and 51 us last.  64 sequences of up to 1024 own tokens behind
-// 8192, 8 KV heads of 128 for 4 query heads each: 57 us with the join, where
-// the two kinds one after another take 41 and 27 us.
+// 8192, 8 KV heads of 128 for 4 query heads each: 60 us, where the two
+// kinds one after another take 41 and 27 us.
 template <int D, bool E4M3, Within WITHIN>
 __global__ void __launch_bounds__(512, 2) k_attend_both(Args a, uint32_t prefix_items, bool prefix_first) {
   __shared__ union {
