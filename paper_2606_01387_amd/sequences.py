@@ -59,7 +59,7 @@ class Sequences:
                            refs=refs.data_ptr(), work=self._scratch.data_ptr())
         self._seqs_ref = ctypes.addressof(self._seqs)
         self._state = (tables, lengths, refs, self._scratch)
-        self._work, self._work_at, self._work_bytes = None, 0, 0
+        self._works, self._work_at, self._work_bytes = [], 0, 0
         self._desc = ctypes.create_string_buffer(_ATTEND.size)
         self._desc_at = ctypes.addressof(self._desc)
         self._device, self._bf16, self._int32 = dev, torch.bfloat16, torch.int32
@@ -129,8 +129,9 @@ class Sequences:
         sequences' last tokens (as in :meth:`write`, which comes first).
         ``scale`` defaults to head_dim ** -0.5.  Returns ``out``.
 
-        The first call of a shape allocates scratch (so it comes before a
-        graph capture of that shape); later ones use it again."""
+        The first call of a shape may allocate scratch (so it comes before a
+        graph capture of that shape); later ones use it again.  Scratch stays
+        where it is, and with it a captured graph, as long as this object does."""
         return self._attend(layer, q, None, 0, 0, ids, offsets, scale, k_scale, v_scale, out)
 
     def attend_shared(self, layer: int, q, prefix, *, ids=None, offsets=None,
@@ -162,12 +163,14 @@ class Sequences:
                 need = ctypes.c_uint64()
                 _check(self._lib.claim_attend_work(pool._h, self._seqs_ref, self._desc_at,
                                                ctypes.byref(need)), "claim_attend_work")
-                # memory of the pool's stream: what was queued there may use
-                # the smaller one until it is done
+                # the smaller ones are kept: a captured graph holds their
+                # addresses.  Each is at least twice the one before, so all of
+                # them together are less than four times what was needed
+                size = max(need.value, 2 * self._work_bytes)
                 torch = _torch()
                 with torch.cuda.stream(pool.stream):
-                    self._work = torch.empty(need.value, dtype=torch.uint8, device=self._device)
-                self._work_at, self._work_bytes = self._work.data_ptr(), need.value
+                    self._works.append(torch.empty(size, dtype=torch.uint8, device=self._device))
+                self._work_at, self._work_bytes = self._works[-1].data_ptr(), size
                 _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
                 rc = self._lib.claim_attend(pool._h, self._seqs_ref, self._desc_at)
             if rc != OK:

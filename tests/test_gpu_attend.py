@@ -286,3 +286,29 @@ def test_a_long_prefix_of_many_rows(torch, ck, block_size, dim, e4m3, group, tim
     w = World(torch, seqs=seqs, heads=1, group=group, dim=dim, block_size=block_size, e4m3=e4m3,
               prefix_blocks=5600 // block_size, seed=21)
     check(attend(ck, w, prefix=True), *w.expected())
+
+
+def test_a_graph_outlives_larger_calls(torch, ck):
+    """A captured step keeps its scratch when a later call takes more of it."""
+    w = World(torch, seqs=[(1, 700), (1, 40)], heads=2, group=4, dim=128, prefix_blocks=20, seed=27)
+    stream = torch.cuda.Stream()
+    pool, seqs, d = w.to_gpu(ck, stream)
+    with pool, torch.cuda.stream(stream):
+        eager = seqs.attend_shared(w.layer, d.q, d.prefix)  # sizes the scratch
+        size = seqs._work_bytes
+        assert size > 0
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = seqs.attend_shared(w.layer, d.q, d.prefix)
+        wide = d.q[:, :1].repeat(1, 64, 1)  # 32 query heads to a KV head
+        for heads in (16, 32, 64):
+            seqs.attend_shared(w.layer, wide[:, :heads].contiguous(), d.prefix)
+        assert seqs._work_bytes > size
+        others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(16)]
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager)
+            assert all(bool((x == 0x5A).all()) for x in others)
+        check(eager, *w.expected())
