@@ -638,7 +638,7 @@ typedef struct claim_attend_desc {
   uint32_t num_heads;
   uint32_t prefix_blocks;
   const uint32_t* prefix; /* [prefix_blocks] */
-  float scale;            /* finite */
+  float scale;            /* above 0, finite, also times k_scale */
   uint32_t reserved;      /* must be 0 */
   void* work;
   uint64_t work_bytes;
