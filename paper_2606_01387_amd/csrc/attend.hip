@@ -61,7 +61,7 @@ struct Args {
   float margin;   // a maximum is followed once scores pass it by 2^8
   float v_scale;
   // parts
-  uint32_t own_splits, prefix_splits, tiles, prefix_tiles;
+  uint32_t own_splits, prefix_splits, tiles;
   float* part_o;   // [row][query head][split][dim]
   float2* part_ml;  // [row][query head][split]: maximum, sum
 };
@@ -1729,7 +1729,6 @@ int claim_attend(claim_pool* P, const claim_seqs* s, const claim_attend_desc* d)
   a.own_splits = plan.own_splits;
   a.prefix_splits = plan.prefix_splits;
   a.tiles = plan.tiles;
-  a.prefix_tiles = plan.prefix_tiles;
   if (plan.parts) {
     a.part_ml = (float2*)d->work;
     a.part_o = (float*)((uint8_t*)d->work + ((plan.parts * sizeof(float2) + 255) & ~255ull));
