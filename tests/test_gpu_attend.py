@@ -312,3 +312,35 @@ def test_a_graph_outlives_larger_calls(torch, ck):
             assert torch.equal(out, eager)
             assert all(bool((x == 0x5A).all()) for x in others)
         check(eager, *w.expected())
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("seqs", [[(90, 10)], [(4, 60)], [(12, 60), (1, 3)]], ids=str)
+def test_hidden_nans_of_both_types(torch, ck, seqs, dim, e4m3):
+    """NaN in a key and in a value that only the last row of a sequence sees."""
+    w = World(torch, seqs=seqs, dim=dim, group=4, e4m3=e4m3, seed=28)
+    clean, bound = w.expected()
+    pos = w.length[0] - 1
+    raw = w.kv.view(torch.uint8) if e4m3 else w.kv
+    raw[2 * w.layer, w.tables[0, pos // w.bs], pos % w.bs, 0, 3] = 0x7F if e4m3 else float("nan")
+    raw[2 * w.layer + 1, w.tables[0, pos // w.bs], pos % w.bs, 1, dim - 1] = 0xFF if e4m3 else float("nan")
+    row = w.seqs[0][0] - 1
+    clean[row, :w.group] = np.nan  # its heads of the first KV head
+    clean[row, w.group:, dim - 1] = np.nan  # one column of the second's
+    check(attend(ck, w), clean, bound)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_hidden_nans_behind_a_prefix(torch, ck, dim, e4m3):
+    """The prefix is longer than one of its sequences, which does not see the NaN."""
+    w = World(torch, seqs=[(1, 20), (1, 0), (1, 7)], dim=dim, group=4, e4m3=e4m3, prefix_blocks=6, seed=29)
+    short = 6 * w.bs - 5
+    w.length[1] = short
+    w.lengths[1] = short
+    clean, bound = w.expected()
+    raw = w.kv.view(torch.uint8) if e4m3 else w.kv
+    raw[2 * w.layer + 1, w.prefix[5], w.bs - 2, 0, 1] = 0x7F if e4m3 else float("nan")
+    clean[0, :w.group, 1] = clean[2, :w.group, 1] = np.nan
+    check(attend(ck, w, prefix=True), clean, bound)
