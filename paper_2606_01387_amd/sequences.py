@@ -32,7 +32,9 @@ class Sequences:
 
     ``tables`` [max_seqs, max_blocks], ``lengths`` [max_seqs] and ``refs``
     [num_blocks] are int32 device tensors that the calls change in place;
-    without them, empty ones are made (max_seqs and max_blocks given)."""
+    without them, empty ones are made (max_seqs and max_blocks given).  They
+    belong to the stream that is current here, and are filled before the pool's
+    stream goes on."""
 
     def __init__(self, pool: claimkv.Pool, max_seqs: int | None = None, max_blocks: int | None = None,
                  *, tables=None, lengths=None, refs=None):
@@ -59,6 +61,11 @@ class Sequences:
                            refs=refs.data_ptr(), work=self._scratch.data_ptr())
         self._seqs_ref = ctypes.addressof(self._seqs)
         self._state = (tables, lengths, refs, self._scratch)
+        if pool._current_stream(pool._device_index) != pool._stream_at:
+            # the tensors belong to the current stream: the pool's waits until they
+            # are filled, and their memory for the pool's work when they are dropped
+            pool.stream.wait_stream(torch.cuda.current_stream(dev))
+            self.record_stream(pool.stream)
         self._works, self._work_at, self._work_bytes = [], 0, 0
         self._desc = ctypes.create_string_buffer(_ATTEND.size)
         self._desc_at = ctypes.addressof(self._desc)
