@@ -32,7 +32,8 @@ class Sequences:
 
     ``tables`` [max_seqs, max_blocks], ``lengths`` [max_seqs] and ``refs``
     [num_blocks] are int32 device tensors that the calls change in place;
-    without them, empty ones are made (max_seqs and max_blocks given).  They
+    without them, empty ones are made (max_seqs and max_blocks given).  Tables
+    come with their lengths; without refs, those count the tables' entries.  They
     belong to the stream that is current here, and are filled before the pool's
     stream goes on."""
 
@@ -44,13 +45,19 @@ class Sequences:
             if not max_seqs or not max_blocks:
                 raise ValueError("max_seqs and max_blocks (or tables) are needed")
             tables = torch.full((max_seqs, max_blocks), NONE, dtype=torch.int32, device=dev)
+            if lengths is None:
+                lengths = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
         if tables.dim() != 2 or tables.numel() == 0:
             raise ValueError("tables must be [max_seqs, max_blocks]")
         if lengths is None:
-            lengths = torch.zeros(tables.shape[0], dtype=torch.int32, device=dev)
-        if refs is None:
-            refs = torch.zeros(g.num_blocks, dtype=torch.int32, device=dev)
+            raise ValueError("tables need their lengths")
         claimkv._device_ints(dev, tables=tables, lengths=lengths, refs=refs)
+        if refs is None:
+            # a block that a table names is not free; other entries count for none
+            named = tables.flatten().long()
+            named = named.where((named >= 0) & (named < g.num_blocks), g.num_blocks)
+            refs = torch.zeros(g.num_blocks + 1, dtype=torch.int32, device=dev)
+            refs = refs.scatter_add_(0, named, torch.ones_like(named, dtype=torch.int32))[:-1]
         if lengths.numel() != tables.shape[0] or refs.numel() != g.num_blocks:
             raise ValueError("lengths needs one entry per sequence, refs one per block")
         self.pool, self.tables, self.lengths, self.refs = pool, tables, lengths, refs
