@@ -520,8 +520,8 @@ const char* claim_strerror(int status);
  * block; entries past its last block are CLAIM_NONE.  refs[b] counts the
  * table entries that name block b, at most 2^31 - 1: a block with refs 0 is
  * free.  A program starts with tables all CLAIM_NONE, lengths and refs 0, and
- * may hold blocks of its own (a claim's, until it is restored) by a count in
- * refs.
+ * may hold blocks of its own (a claim's, until it is restored; a prefix list's)
+ * by a count more in refs: held blocks are neither handed out nor moved.
  *
  * A block handed out (by grow, fork, compact) no longer holds the cache
  * identity it was registered with: claim_lookup does not hit it.  A claim
@@ -560,8 +560,11 @@ typedef struct claim_seqs {
  *                   row named twice, or out of range, is passed over.
  * claim_seqs_compact moves the blocks in use to the front of the pool: with
  *                   U blocks in use, the i-th used block from U on (ascending)
- *                   moves into the i-th free block below U; tables and refs
- *                   follow.  *moved (device, may be NULL) = blocks moved.
+ *                   that is not held moves into the i-th free block below U;
+ *                   tables and refs follow.  A block is held if it has more
+ *                   counts than table entries that name it: what names it from
+ *                   outside the tables (a claim, a list given as `prefix`) would
+ *                   not follow.  *moved (device, may be NULL) = blocks moved.
  *                   Claims name physical blocks: a claim whose blocks moved
  *                   no longer finds its bytes there and fails closed.
  * claim_blocks_copy copies block src[i] over block dst[i] in every plane.  No

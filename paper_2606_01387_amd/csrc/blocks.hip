@@ -498,33 +498,73 @@ __global__ void __launch_bounds__(kCopy) k_free(Seqs s, const uint32_t* ids, uin
 
 // ------------------------------------------------------------------- compact
 
+// How many table entries name each block, as a block with more counts than that is
+// held by the program and stays where it is: a claim's or a prefix list's blocks are
+// named from outside the tables.  The plan counts in LDS where the pool and the
+// tables are small, else two launches ahead of it count in scratch: with nothing to
+// move, 64 blocks and entries 5.5 us in the plan and 8.3 in launches, 8000 blocks and
+// 8192 entries 8.2 and 10.1, 16000 and 16384 11.5 and 11.6.
+constexpr uint32_t kCounted = 8192;  // blocks, and table entries, that the plan counts itself
+
+__host__ __device__ inline bool plan_counts(uint32_t nb, uint32_t max_seqs, uint32_t max_blocks) {
+  return nb <= kCounted && (uint64_t)max_seqs * max_blocks <= kCounted;
+}
+
+__global__ void __launch_bounds__(kCopy) k_count_none(uint32_t* counts, uint32_t nb) {
+  for (uint64_t b = (uint64_t)blockIdx.x * kCopy + threadIdx.x; b < nb; b += (uint64_t)gridDim.x * kCopy)
+    counts[b] = 0;
+}
+
+__global__ void __launch_bounds__(kCopy) k_count_entries(Seqs s, uint32_t nb) {
+  const uint64_t entries = (uint64_t)s.max_seqs * s.max_blocks;
+  for (uint64_t i = (uint64_t)blockIdx.x * kCopy + threadIdx.x; i < entries;
+       i += (uint64_t)gridDim.x * kCopy) {
+    const uint32_t b = s.tables[i];
+    if (b < nb) atomicAdd(&s.map[b], 1u);
+  }
+}
+
 // Which blocks move, as the header defines it: U blocks in use, those of them at
-// or past U in `list_b`, the free ones below U in `list_a`, pair by pair.  Bound by
-// dependent reads: 2000 blocks in 5.3 us.
+// or past U that are not held in `list_b`, the first free ones below U in `list_a`,
+// pair by pair.  COUNT: entries are counted here, else `map` has their numbers.
+// Bound by dependent reads: 2000 blocks in 5.3 us.
+template <bool COUNT>
 __global__ void __launch_bounds__(kPlan) k_compact_plan(Seqs s, uint32_t nb, uint64_t* holder,
                                                         uint32_t* moved) {
-  __shared__ uint32_t used_below;  // blocks in use below U
+  __shared__ uint32_t counts[COUNT ? kCounted : 1];
   const Share share = my_share(s.refs, nb);
+  if (COUNT) {
+    for (uint32_t b = threadIdx.x; b < nb; b += kPlan) counts[b] = 0;
+    __syncthreads();
+    const uint32_t entries = s.max_seqs * s.max_blocks;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < entries; i += kPlan) {
+      const uint32_t b = s.tables[i];
+      if (b < nb) atomicAdd(&counts[b], 1u);
+    }
+    __syncthreads();
+  }
+  const auto movable = [&](uint32_t b) { return s.refs[b] <= (COUNT ? counts[b] : s.map[b]); };
   uint64_t total;
   const uint32_t before = (uint32_t)block_scan(share.used, &total);
   const uint32_t U = (uint32_t)total;
-  if (threadIdx.x == 0) used_below = U;  // U = nb: nobody's share holds block U
-  __syncthreads();
-  if (share.first <= U && U < share.last) {
-    uint32_t low = before;
-    for (uint32_t b = share.first; b < U; ++b) low += in_use(share, s.refs, b);
-    used_below = low;
-  }
-  __syncthreads();
-  const uint32_t low = used_below, pairs = U - low;
+  // blocks that move, in order
+  uint32_t mine = 0;
+  for (uint32_t b = share.first > U ? share.first : U; b < share.last; ++b)
+    mine += in_use(share, s.refs, b) && movable(b);
+  uint64_t pairs_all;
+  uint32_t at = (uint32_t)block_scan(mine, &pairs_all);
+  const uint32_t pairs = (uint32_t)pairs_all;
   uint32_t used = before;
   for (uint32_t b = share.first; b < share.last; ++b) {
     const bool taken = in_use(share, s.refs, b);
     if (b < U) {
-      if (!taken) s.list_a[b - used] = b;
+      if (!taken) s.list_a[b - used] = b;  // at least `pairs` of them: U less those in use below U
     } else {
-      s.map[b] = kNone;  // an entry that names a block with no count names nothing
-      if (taken) s.list_b[used - low] = b;
+      const bool moves = taken && movable(b);
+      // an entry that names a block with no count names nothing
+      s.map[b] = taken ? b : kNone;
+      if (moves) s.list_b[at++] = b;
     }
     used += taken;
   }
@@ -759,7 +799,15 @@ int claim_seqs_compact(claim_pool* P, const claim_seqs* s, uint32_t* moved) {
   const PoolView p = pool_view(P);
   SEQ_HIP(hipSetDevice(p.device));
   const Seqs d = seqs_dev(s, p.nb);
-  hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kPlan), 0, p.stream, d, p.nb, p.holder, moved);
+  if (plan_counts(p.nb, s->max_seqs, s->max_blocks)) {
+    hipLaunchKernelGGL(k_compact_plan<true>, dim3(1), dim3(kPlan), 0, p.stream, d, p.nb, p.holder, moved);
+  } else {
+    const uint64_t blocks = ((uint64_t)p.nb + kCopy - 1) / kCopy;
+    const uint64_t entries = ((uint64_t)s->max_seqs * s->max_blocks + kCopy - 1) / kCopy;
+    hipLaunchKernelGGL(k_count_none, dim3(copy_grid(p, blocks)), dim3(kCopy), 0, p.stream, d.map, p.nb);
+    hipLaunchKernelGGL(k_count_entries, dim3(copy_grid(p, entries)), dim3(kCopy), 0, p.stream, d, p.nb);
+    hipLaunchKernelGGL(k_compact_plan<false>, dim3(1), dim3(kPlan), 0, p.stream, d, p.nb, p.holder, moved);
+  }
   const CopyShape c = copy_shape(p);
   const uint64_t most = (uint64_t)(p.nb / 2 + 1) * c.planes * c.pieces;
   hipLaunchKernelGGL(k_compact_apply, dim3(copy_grid(p, most)), dim3(kCopy), 0, p.stream, d, c,

@@ -110,8 +110,10 @@ class Sequences:
             _check(self._lib.claim_seqs_free(pool._h, self._seqs_ref, at, ids.numel()), "claim_seqs_free")
 
     def compact(self):
-        """claim_seqs_compact: blocks in use move to the front of the pool.
-        Returns the device tensor [1] of how many moved."""
+        """claim_seqs_compact: blocks in use move to the front of the pool, but
+        for those that the program holds by a count of its own in ``refs`` (a
+        ``prefix`` of :meth:`attend_shared`, a claim's blocks).  Returns the
+        device tensor [1] of how many moved."""
         pool = self.pool
         moved = self.refs.new_empty(1)
         with pool.ordered(self, moved):
@@ -153,7 +155,9 @@ class Sequences:
                       out=None):
         """:meth:`attend` for sequences that all begin with the whole blocks
         ``prefix`` (int32 device tensor), which are read once for all of them;
-        the tables' own entries for those positions are not read."""
+        the tables' own entries for those positions are not read.  A list that
+        is kept over a :meth:`compact` needs a count more of its blocks in
+        ``refs``, or they may move."""
         return self._attend(layer, q, prefix, self._ints("prefix", prefix), prefix.numel(), ids,
                             offsets, scale, k_scale, v_scale, out)
 
