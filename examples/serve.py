@@ -126,10 +126,9 @@ def serve(prompt=300, samples=6, steps=20, blocks=256, block_size=16, group=2, v
         left = int((seqs.refs > 0).sum())
         report["left"] = left
         report["packed"] = bool((seqs.refs[:left] > 0).all())
-        # a claim names blocks: after they were freed and handed out again, or
-        # moved, it is judged by its own record and fails closed
-        if report["moved"]:
-            report["hit_blocks_after"] = int(pool.lookup(batch)["hit_blocks"][0])
+        # the claim names blocks: the kept samples share the full ones; the last one was
+        # freed, and what moved into its place is not the claim's
+        report["hit_blocks_after"] = int(pool.lookup(batch)["hit_blocks"][0])
         report["said"] = said.cpu().numpy()
     return report
 

@@ -565,8 +565,11 @@ typedef struct claim_seqs {
  *                   counts than table entries that name it: what names it from
  *                   outside the tables (a claim, a list given as `prefix`) would
  *                   not follow.  *moved (device, may be NULL) = blocks moved.
- *                   Claims name physical blocks: a claim whose blocks moved
- *                   no longer finds its bytes there and fails closed.
+ *                   Claims name physical blocks and stay with them: where a
+ *                   block moved from, its bytes and identity are left, as in a
+ *                   freed block, so that lookups hit and checks pass until the
+ *                   block is handed out again and written; then they miss and
+ *                   fail closed.
  * claim_blocks_copy copies block src[i] over block dst[i] in every plane.  No
  *                   block may be written twice, or both written and read, in
  *                   one call; pairs with a block >= num_blocks are passed over.
