@@ -225,8 +225,9 @@ __global__ void __launch_bounds__(kPlan) k_grow(Seqs s, const uint32_t* ids, con
     uint64_t total;
     const uint64_t at = run + block_scan(fine ? need : 0, &total);
     if (i < n) {
-      // ranks past the blocks there are stay past them in 32 bits
-      s.rank[i] = at < nb ? (uint32_t)at : nb;
+      // ranks past the blocks there are stay past them in 32 bits, also where an
+      // entry needs none
+      s.rank[i] = at <= nb ? (uint32_t)at : nb + 1;
       s.need[i] = (uint32_t)need;
     }
     run += total;
