@@ -620,7 +620,8 @@ int claim_kv_write(claim_pool* pool, const claim_seqs* seqs, const claim_kv_desc
  * query head h reads KV head h / (num_heads / num_kv_heads), and the row at
  * position P sees positions 0..P:
  *   out = sum_p w_p v_p / sum_p w_p,  w_p = exp(scale * q . k_p).
- * A row that sees nothing (P < 0) gives 0.  A row that sees a position whose
+ * A row that sees nothing (P < 0) gives 0; one that sees positions whose scores
+ * are all -infinity gives NaN (0 / 0).  A row that sees a position whose
  * block is missing (CLAIM_NONE, >= num_blocks, or past the table) gives NaN:
  * it fails closed.  Positions that a row does not see have no effect on it,
  * whatever bytes they hold.  Scores, weights' sums and outputs are

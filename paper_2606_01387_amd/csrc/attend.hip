@@ -37,6 +37,10 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNoMax = -__builtin_inff();
 
+// A part's maximum where the row sees keys and every score is -infinity: above
+// kNoMax, which is left for rows that see nothing, and no higher than any score.
+constexpr float kLeast = -3.402823466e38f;
+
 // What a row of keys or values reads where there is none: 16 bytes of zeros
 // (positions past the range: their weight is 0, and 0 x 0 adds nothing), then
 // 16 bytes that are NaN in bf16 and in e4m3 (keys of a missing block).
@@ -72,6 +76,10 @@ struct Row {
   uint32_t row, head;  // packed row, query head
   uint32_t limit;      // positions below it are seen
 };
+
+// What the row's results are divided by turns into: 0 for a row that sees nothing.
+// One that sees keys of score -infinity alone has 0 / 0, as its formula does.
+__device__ __forceinline__ float over_sum(float x, float sum, bool sees) { return sees ? x / sum : 0.0f; }
 
 // A value that all lanes of the wave have, for the scalar unit.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -561,12 +569,12 @@ struct Wave {
 
   // The rows' parts for the joining kernel: through LDS of the wave's own (32
   // rows of D floats), so that whole rows are stored at a time.
-  __device__ __forceinline__ void finish_part(const Args& a, const Row& r, uint32_t split, uint32_t splits,
-                                              uint8_t* lds) {
+  __device__ __forceinline__ void finish_part(const Args& a, const Row& r, bool sees, uint32_t split,
+                                              uint32_t splits, uint8_t* lds) {
     const uint32_t lane = threadIdx.x & 63, h = lane >> 5, row = lane & 31;
     const float sum = across_halves_add(l);
     uint64_t at = ((uint64_t)r.row * a.heads * a.group + r.head) * splits + split;
-    if (r.valid && h == 0) a.part_ml[at] = float2{m, sum};
+    if (r.valid && h == 0) a.part_ml[at] = float2{sees ? fmaxf(m, kLeast) : m, sum};
     if (!r.valid || sum == 0.0f) at = ~0ull;
     constexpr uint32_t kChunks = D / 4;  // 16-byte chunks of a row, exchanged by its number
 #pragma unroll
@@ -588,11 +596,11 @@ struct Wave {
   }
 
   // The rows' results.
-  __device__ __forceinline__ void finish(const Args& a, const Row& r) {
+  __device__ __forceinline__ void finish(const Args& a, const Row& r, bool sees) {
     const uint32_t h = (threadIdx.x >> 5) & 1;
     const float sum = across_halves_add(l);
     if (!r.valid) return;
-    const float f = sum == 0.0f ? 0.0f : a.v_scale / sum;
+    const float f = over_sum(a.v_scale, sum, sees);
     uint16_t* dst = a.out + r.row * a.out_row + r.head * a.out_head + 4 * h;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
@@ -1001,15 +1009,16 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
     wait_loads();
     meet();
   }
+  const bool sees = row.limit > lo && hi > lo;
   if (a.part_o) {
     meet();  // the tiles have been read
     constexpr uint32_t kRoom = 32 * D * 4;
     static_assert(WAVES / 2 * kRoom <= 4 * kTile, "");
     const uint32_t wave = uniform(t >> 6);
-    w.finish_part(a, row, prefix ? a.own_splits + split : split, a.own_splits + a.prefix_splits,
+    w.finish_part(a, row, sees, prefix ? a.own_splits + split : split, a.own_splits + a.prefix_splits,
                   wave < WAVES / 2 ? lk + wave * kRoom : lv + (wave - WAVES / 2) * kRoom);
   } else {
-    w.finish(a, row);
+    w.finish(a, row, sees);
   }
 }
 
@@ -1408,15 +1417,16 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
     w.l[c] = 0;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) w.l[c] += sums[i][16 * c + (t & 15)];
+    const bool sees = row[c].limit > it.range.lo && hi > it.range.lo;
     if (a.part_o) {
       const uint64_t to = ((uint64_t)row[c].row * a.heads * a.group + row[c].head) * all +
                           (prefix ? a.own_splits + split : split);
-      if (t < 16) a.part_ml[to] = float2{w.m[c], w.l[c]};
+      if (t < 16) a.part_ml[to] = float2{sees ? fmaxf(w.m[c], kLeast) : w.m[c], w.l[c]};
       if (w.l[c] == 0.0f) continue;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) *(f32x4*)(a.part_o + to * D + 16 * j + g4) = w.o[c][j];
     } else {
-      const float f = w.l[c] == 0.0f ? 0.0f : a.v_scale / w.l[c];
+      const float f = over_sum(a.v_scale, w.l[c], sees);
       uint16_t* dst = a.out + row[c].row * a.out_row + row[c].head * a.out_head + g4;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) {
@@ -1526,7 +1536,7 @@ __global__ void __launch_bounds__(256) k_join(Args a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
   if (lane >= kLanes) return;
-  const float y = l == 0.0f ? 0.0f : a.v_scale / l;
+  const float y = over_sum(a.v_scale, l, m != kNoMax);
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   bf16x4 e;
 #pragma unroll
