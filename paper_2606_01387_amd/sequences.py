@@ -227,4 +227,5 @@ class Sequences:
                 or x.shape[1] != heads or x.shape[2] != dim or stride[2] != 1):
             raise ValueError(f"{name} must be bf16 [rows, {heads}, {dim}] on {self._device}, "
                              "its last dimension contiguous")
-        return x.data_ptr(), stride[0], stride[1]
+        # the stride of a single row or head leads nowhere, and may be anything
+        return x.data_ptr(), stride[0] if x.shape[0] > 1 else 0, stride[1] if heads > 1 else 0
