@@ -626,7 +626,8 @@ int claim_kv_write(claim_pool* pool, const claim_seqs* seqs, const claim_kv_desc
  * it fails closed.  Positions that a row does not see have no effect on it,
  * whatever bytes they hold.  Scores, weights' sums and outputs are
  * accumulated in 32 bits; the weights are rounded to bf16 for the product
- * with V.
+ * with V.  Outputs are divided by their weights' sum at the end, and a weight
+ * may be 2^8 until then: values of 10^30 and more can pass 32 bits.
  *
  * With prefix_blocks > 0, positions 0 .. prefix_blocks * block_size - 1 of
  * every sequence are read from `prefix` (what the tables hold there is not

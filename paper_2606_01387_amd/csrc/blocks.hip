@@ -502,9 +502,10 @@ __global__ void __launch_bounds__(kCopy) k_free(Seqs s, const uint32_t* ids, uin
 // How many table entries name each block, as a block with more counts than that is
 // held by the program and stays where it is: a claim's or a prefix list's blocks are
 // named from outside the tables.  The plan counts in LDS where the pool and the
-// tables are small, else two launches ahead of it count in scratch: with nothing to
-// move, 64 blocks and entries 5.5 us in the plan and 8.3 in launches, 8000 blocks and
-// 8192 entries 8.2 and 10.1, 16000 and 16384 11.5 and 11.6.
+// tables are small, else two launches ahead of it count in scratch.  A compaction that
+// moves nothing, with no count / one in the plan / one in launches: 64 blocks and
+// entries 5.0 / 5.6 / 8.3 us, 2000 blocks and 3120 entries 5.0 / 6.2 / 8.8, 8000 and
+// 8192 6.2 / 8.2 / 10.1, 16000 and 16384 8.5 / 11.5 / 11.6.
 constexpr uint32_t kCounted = 8192;  // blocks, and table entries, that the plan counts itself
 
 __host__ __device__ inline bool plan_counts(uint32_t nb, uint32_t max_seqs, uint32_t max_blocks) {
@@ -528,7 +529,7 @@ __global__ void __launch_bounds__(kCopy) k_count_entries(Seqs s, uint32_t nb) {
 // Which blocks move, as the header defines it: U blocks in use, those of them at
 // or past U that are not held in `list_b`, the first free ones below U in `list_a`,
 // pair by pair.  COUNT: entries are counted here, else `map` has their numbers.
-// Bound by dependent reads: 2000 blocks in 5.3 us.
+// Bound by dependent reads: 2000 blocks and 3120 entries in 7.8 us.
 template <bool COUNT>
 __global__ void __launch_bounds__(kPlan) k_compact_plan(Seqs s, uint32_t nb, uint64_t* holder,
                                                         uint32_t* moved) {

@@ -63,14 +63,19 @@ def test_dropped_behind_work_of_the_pools_stream(torch, ck):
         seqs = Sequences(pool, 1000, 300)
         ids = torch.arange(3, dtype=torch.int32, device="cuda")
         tokens = ids + 20
+        held = {t.data_ptr(): t.numel() for t in (seqs._scratch, seqs.tables)}
+
+        def others():
+            return [torch.empty(n, dtype=torch.int32, device="cuda") for n in held.values() for _ in range(4)]
+
+        others()  # there is room for them, as taking memory from the device may wait
         with torch.cuda.stream(side):
             seqs.grow(ids, tokens)  # kernels are loaded by their first launch
             torch.cuda.synchronize()
             keep_busy(torch, x)
             seqs.grow(ids, tokens)
-        held = {t.data_ptr(): t.numel() for t in (seqs._scratch, seqs.tables)}
         del seqs
-        again = [torch.empty(n, dtype=torch.int32, device="cuda") for n in held.values() for _ in range(4)]
+        again = others()
         busy = not side.query()
         torch.cuda.synchronize()
         assert busy  # else the memory is free by now and nothing was tested
