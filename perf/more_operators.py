@@ -305,7 +305,7 @@ def _run_own(s):
     if s["op"] == "rotate":
         out = q.write_rotated(s["layer"], s["q"], s["k"], s["v"], s["freqs"], positions=s["positions"],
                               sections=s["sections"], q_norm=s["q_norm"], k_norm=s["k_norm"],
-                              interleaved=s.get("interleaved", False), offsets=s["offsets"],
+                              neighbours=s.get("interleaved", False), offsets=s["offsets"],
                               k_scale=s["k_scale"], v_scale=s["v_scale"])
         return out, s["kv"]
     if s["op"] == "window":
