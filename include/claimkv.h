@@ -616,6 +616,47 @@ typedef struct claim_kv_desc {
 int claim_kv_write(claim_pool* pool, const claim_seqs* seqs, const claim_kv_desc* kv,
                    const claim_rows* k, const claim_rows* v);
 
+/* claim_kv_write of keys that a layer still has to norm and turn by their
+ * positions, with the rows' queries.  For each head x of q (num_heads heads) and
+ * of k, with the head's weights w (q_norm, k_norm: bf16 [head_dim], 16-byte aligned;
+ * NULL: y = x):
+ *   y = x w / sqrt(mean(x^2) + eps);
+ *   pair i < rot_dims / 2 of it, (a, b) = (y[i], y[i + rot_dims / 2]), or with
+ *   CLAIM_ROTATE_NEIGHBOURS (y[2 i], y[2 i + 1]), becomes
+ *   (a cos t - b sin t, b cos t + a sin t) with t = position * freqs[i].
+ * The position of pair i in row r is positions[r * position_stride + axis *
+ * axis_stride] (text, or time, height and width), where the first sections[0]
+ * pairs belong to axis 0, the next sections[1] to axis 1 and so on, and the
+ * sections add up to rot_dims / 2; only entries of axes that have pairs are read.
+ * Without positions (NULL) it is the row's position in its sequence, which a
+ * program whose caches are cut cannot use.  All of it is computed in 32 bits
+ * (angles in 64; squares past 10^38 are infinite) and rounded once: queries to
+ * bf16 in out, which may be q, keys and values as claim_kv_write does.  A row
+ * whose position has no block is not written into the pool, but its queries are
+ * given; a row that offsets give to no sequence leaves out as it was.
+ *
+ * head_dim is 64 or 128, rot_dims a multiple of 16 up to head_dim (0: norms
+ * alone), num_rows x num_heads below 2^26, eps at least 0, else EINVAL. */
+#define CLAIM_ROTATE_NEIGHBOURS 0x1u
+typedef struct claim_rotate_desc {
+  claim_kv_desc kv;
+  claim_rows q, k, v;
+  claim_rows out;
+  uint32_t num_heads; /* query heads */
+  uint32_t rot_dims;
+  const double* freqs;      /* [rot_dims / 2] radians a position */
+  const int32_t* positions; /* or NULL */
+  uint64_t position_stride; /* in entries, from row to row */
+  uint64_t axis_stride;     /* from axis to axis */
+  uint32_t sections[4];
+  const void* q_norm;
+  const void* k_norm;
+  float eps;
+  uint32_t flags; /* CLAIM_ROTATE_NEIGHBOURS */
+} claim_rotate_desc;
+
+int claim_kv_write_rotated(claim_pool* pool, const claim_seqs* seqs, const claim_rotate_desc* desc);
+
 /* Attention of the rows' queries over their sequences' keys and values:
  * query head h reads KV head h / (num_heads / num_kv_heads), and the row at
  * position P sees positions 0..P:

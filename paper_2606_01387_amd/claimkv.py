@@ -16,7 +16,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SOURCE = os.path.join(_HERE, "csrc", "claimkv.hip")
-SOURCES = (SOURCE, os.path.join(_HERE, "csrc", "blocks.hip"), os.path.join(_HERE, "csrc", "attend.hip"))
+SOURCES = (SOURCE, *(os.path.join(_HERE, "csrc", name + ".hip") for name in ("blocks", "attend", "rotate")))
 LIBRARY = os.path.join(_HERE, "libclaimkv.so")
 INCLUDE = os.path.join(ROOT, "include")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -57,7 +57,7 @@ EXPORTS = ("claim_pool_create", "claim_pool_destroy", "claim_offload", "claim_re
            "claim_identity_stats", "outcomes_read", "claim_timing_read", "claim_block_state_read",
            "claim_digest_grid", "claim_strerror", "claim_seqs_grow", "claim_seqs_fork",
            "claim_seqs_free", "claim_seqs_compact", "claim_blocks_copy", "claim_kv_write",
-           "claim_attend", "claim_attend_work")
+           "claim_kv_write_rotated", "claim_attend", "claim_attend_work")
 
 
 class PoolDesc(ctypes.Structure):
@@ -115,6 +115,15 @@ class CKvDesc(ctypes.Structure):
                 ("num_rows", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
                 ("ids", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
                 ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
+class CRotateDesc(ctypes.Structure):
+    _fields_ = [("kv", CKvDesc), ("q", CRows), ("k", CRows), ("v", CRows), ("out", CRows),
+                ("num_heads", ctypes.c_uint32), ("rot_dims", ctypes.c_uint32),
+                ("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("position_stride", ctypes.c_uint64), ("axis_stride", ctypes.c_uint64),
+                ("sections", ctypes.c_uint32 * 4), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 class CAttendDesc(ctypes.Structure):
@@ -180,6 +189,7 @@ def lib() -> ctypes.CDLL:
             "claim_seqs_compact": ([vp, vp, vp], i32),
             "claim_blocks_copy": ([vp, vp, vp, u32], i32),
             "claim_kv_write": ([vp, vp, vp, vp, vp], i32),
+            "claim_kv_write_rotated": ([vp, vp, vp], i32),
             "claim_attend": ([vp, vp, vp], i32),
             "claim_attend_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
         }

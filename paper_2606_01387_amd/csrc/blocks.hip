@@ -8,15 +8,13 @@
 // host.
 
 #include "pool_view.h"
+#include "write_row.h"
 
 namespace {
 
 constexpr uint32_t kNone = CLAIM_NONE;
 constexpr int kPlan = 1024;  // threads of a planning workgroup
 constexpr int kCopy = 256;   // threads of a copying workgroup
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Seqs {
   uint32_t max_seqs, max_blocks;
@@ -613,52 +611,6 @@ struct WriteArgs {
   uint32_t token_bytes;
   uint8_t *k_plane, *v_plane;
 };
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-// x / scale, rounded as a division is, limited to the largest e4m3 value; NaN
-// passes through.  q = x (1 / scale) is off by an ulp or two at most; the
-// remainder x - q scale is exact in one fused step, and so corrects it to the
-// nearest value (Markstein's division; inverse is 1 / scale rounded to nearest).
-// q is kept finite so that the remainder of an overflow is no NaN: it is past
-// the limit anyway.  24 prompts of 100 to 1500 rows of 4 heads of 128: 18.8 us
-// with the compiler's division, 15.3 us so.
-__device__ __forceinline__ float limit_e4m3(float x, float scale, float inverse) {
-  const float q = __builtin_amdgcn_fmed3f(x * inverse, -1000.0f, 1000.0f);
-  const float y = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
-  const float z = __builtin_amdgcn_fmed3f(y, -448.0f, 448.0f);
-  return x != x ? x : z;
-}
-
-// Four bf16 values (two words) to four e4m3 bytes, to nearest even.
-__device__ __forceinline__ uint32_t to_e4m3(uint32_t w0, uint32_t w1, float scale, float inverse) {
-  int p = __builtin_amdgcn_cvt_pk_fp8_f32(limit_e4m3(bf16_lo(w0), scale, inverse),
-                                          limit_e4m3(bf16_hi(w0), scale, inverse), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(limit_e4m3(bf16_lo(w1), scale, inverse),
-                                                   limit_e4m3(bf16_hi(w1), scale, inverse), p, true);
-}
-
-// Where a packed row goes: the byte of its token in a plane, or false.
-__device__ __forceinline__ bool find_row(const WriteArgs& a, const Seqs& s, uint32_t row, uint64_t* token_at) {
-  uint32_t q = row, i = 0, n = 1;
-  if (a.offsets) {
-    q = wave_find_seq(a.offsets, a.num_seqs, row);
-    const uint32_t o = a.offsets[q], e = a.offsets[q + 1];
-    if (o > row || e <= row) return false;  // offsets that do not hold the row
-    i = row - o;
-    n = e - o;
-  }
-  const uint32_t r = a.ids ? a.ids[q] : q;
-  if (r >= s.max_seqs) return false;
-  const int64_t pos = (int64_t)s.lengths[r] - n + i;
-  if (pos < 0) return false;
-  const uint32_t at = (uint32_t)pos / a.bs, token = (uint32_t)pos % a.bs;
-  if (at >= s.max_blocks) return false;
-  const uint32_t b = s.tables[(uint64_t)r * s.max_blocks + at];
-  *token_at = (uint64_t)b * a.chunk_bytes + (uint64_t)token * a.token_bytes;
-  return b < a.nb;
-}
 
 // A wave takes one row; its lanes take the row's 16-byte vectors, first K's,
 // then V's, four each at a time.  The first of them are asked for before the

@@ -14,17 +14,19 @@ import ctypes
 import struct
 
 from . import claimkv
-from .claimkv import CAttendDesc, CKvDesc, CRows, CSeqs, ENOSPC, OK, _check, _torch, lib
+from .claimkv import CAttendDesc, CKvDesc, CRotateDesc, CRows, CSeqs, ENOSPC, OK, _check, _torch, lib
 
 SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED = 0, 1, 2
 NONE = -1  # a table entry that names no block (0xFFFFFFFF in 32 bits)
 
-# claim_kv_desc with two claim_rows after it, and claim_attend_desc, packed in
+# claim_kv_desc with two claim_rows after it, and the other descriptions, packed in
 # one step: filling them field by field takes longer than queueing the work
 _WRITE = struct.Struct("<4I2Q2f6Q")
 _ATTEND = struct.Struct("<4I2Q2f6Q2IQfI2Q")
 assert _WRITE.size == ctypes.sizeof(CKvDesc) + 2 * ctypes.sizeof(CRows)
+_ROTATE = struct.Struct("<4I2Q2f12Q2I4Q4I2QfI")
 assert _ATTEND.size == ctypes.sizeof(CAttendDesc)
+assert _ROTATE.size == ctypes.sizeof(CRotateDesc)
 
 
 class Sequences:
@@ -74,9 +76,10 @@ class Sequences:
             pool.stream.wait_stream(torch.cuda.current_stream(dev))
             self.record_stream(pool.stream)
         self._works, self._work_at, self._work_bytes = [], 0, 0
-        self._desc = ctypes.create_string_buffer(_ATTEND.size)
+        self._desc = ctypes.create_string_buffer(max(_ATTEND.size, _ROTATE.size))
         self._desc_at = ctypes.addressof(self._desc)
         self._device, self._bf16, self._int32 = dev, torch.bfloat16, torch.int32
+        self._float64 = torch.float64
         self._heads, self._dim = g.num_kv_heads, g.head_dim
         self._lib = lib()
 
@@ -137,6 +140,62 @@ class Sequences:
         with pool.ordered(self, k, v, ids, offsets):
             _check(self._lib.claim_kv_write(pool._h, self._seqs_ref, at, at + 40, at + 64),
                    "claim_kv_write")
+
+    def write_rotated(self, layer: int, q, k, v, freqs, *, positions=None, sections=None, q_norm=None,
+                      k_norm=None, eps: float = 1e-6, neighbours: bool = False, ids=None, offsets=None,
+                      k_scale: float = 1.0, v_scale: float = 1.0, out=None):
+        """claim_kv_write_rotated: :meth:`write` of keys that are first normed by
+        head and turned by their positions, as ``q`` ([rows, heads, head_dim],
+        bf16) is.  Returns ``out``, the queries for :meth:`attend` (it may be
+        ``q``).
+
+        ``freqs`` (float64 [pairs], radians a position; None: nothing turns)
+        belong to the pairs (i, i + pairs) of a head, or with ``neighbours`` (2 i,
+        2 i + 1).  ``positions`` (int32 [rows] or [rows, axes], up to 4) are the
+        rows' positions, each axis's that of ``sections[axis]`` pairs in turn;
+        without them, rows have their positions in their sequences.  ``q_norm``
+        and ``k_norm`` (bf16 [head_dim]) are the weights of x w / sqrt(mean(x^2)
+        + eps); None leaves heads as they are."""
+        pool, shape = self.pool, q.shape
+        if len(shape) != 3 or k.shape[0] != shape[0] or v.shape[0] != shape[0]:
+            raise ValueError("q must be [rows, heads, head_dim], and k and v have the same rows")
+        rows, heads = shape[0], shape[1]
+        given = (*self._rows("q", q, heads), *self._rows("k", k, self._heads),
+                 *self._rows("v", v, self._heads))
+        if out is None:
+            out = q.new_empty(shape)
+        elif out.shape != shape:
+            raise ValueError("out needs q's shape")
+        pairs = 0 if freqs is None else freqs.numel()
+        if pairs and (freqs.dtype != self._float64 or freqs.device != self._device
+                      or not freqs.is_contiguous()):
+            raise ValueError(f"freqs must be a contiguous float64 tensor on {self._device}")
+        sections = (pairs,) if sections is None else tuple(sections)
+        at, row_stride, axis_stride = 0, 0, 0
+        if positions is not None:
+            axes = positions.shape[1] if positions.dim() == 2 else 1
+            if (positions.dtype != self._int32 or positions.device != self._device
+                    or positions.dim() not in (1, 2) or positions.shape[0] != rows):
+                raise ValueError(f"positions must be int32 [rows] or [rows, axes] on {self._device}")
+            if axes != len(sections):
+                raise ValueError("positions need as many axes as sections")
+            at, row_stride = positions.data_ptr(), positions.stride(0)
+            axis_stride = positions.stride(1) if positions.dim() == 2 else 0
+        if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != pairs:
+            raise ValueError("sections must be up to 4 numbers of pairs that add up to freqs'")
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None and (w.dtype != self._bf16 or w.device != self._device
+                                  or w.numel() != self._dim or not w.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous bf16 [{self._dim}] on {self._device}")
+        _ROTATE.pack_into(self._desc, 0, *self._kv(layer, rows, ids, offsets), k_scale, v_scale, *given,
+                          *self._rows("out", out, heads), heads, 2 * pairs,
+                          freqs.data_ptr() if pairs else 0, at, row_stride, axis_stride,
+                          *(sections + (0, 0, 0))[:4], 0 if q_norm is None else q_norm.data_ptr(),
+                          0 if k_norm is None else k_norm.data_ptr(), eps, 1 if neighbours else 0)
+        with pool.ordered(self, q, k, v, out, freqs, positions, q_norm, k_norm, ids, offsets):
+            _check(self._lib.claim_kv_write_rotated(pool._h, self._seqs_ref, self._desc_at),
+                   "claim_kv_write_rotated")
+        return out
 
     def attend(self, layer: int, q, *, ids=None, offsets=None, scale: float | None = None,
                k_scale: float = 1.0, v_scale: float = 1.0, out=None):
