@@ -697,6 +697,27 @@ int claim_attend_work(const claim_pool* pool, const claim_seqs* seqs, const clai
                       uint64_t* bytes);
 int claim_attend(claim_pool* pool, const claim_seqs* seqs, const claim_attend_desc* desc);
 
+/* claim_attend in a sliding window: the row at position P sees positions P -
+ * window + 1 .. P and the first ones, 0 .. sinks - 1 (those up to P).  Only blocks
+ * of positions that some row sees are read: entries behind the window may be
+ * CLAIM_NONE.  window is at least 1 (2^32 - 1: all positions), prefix_blocks 0 and
+ * prefix NULL; everything else is as claim_attend has it.
+ *
+ * With lse (float [num_rows][num_heads], may be NULL) each row's and head's
+ * logarithm of sum_p exp(scale * k_scale * q . k_p) is written there, for
+ * claim_weigh: -infinity where nothing is seen, NaN where the output is NaN for a
+ * missing block or a score that is NaN or +infinity. */
+typedef struct claim_window_desc {
+  claim_attend_desc attend; /* work: claim_attend_window_work bytes */
+  uint32_t window;
+  uint32_t sinks;
+  float* lse;
+} claim_window_desc;
+
+int claim_attend_window_work(const claim_pool* pool, const claim_seqs* seqs, const claim_window_desc* desc,
+                             uint64_t* bytes);
+int claim_attend_window(claim_pool* pool, const claim_seqs* seqs, const claim_window_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

@@ -116,22 +116,6 @@ uint64_t plan_bytes(const Plan& r, uint32_t dim) {
   return r.parts ? ((r.parts * sizeof(float2) + 255) & ~255ull) + r.parts * dim * sizeof(float) : 0;
 }
 
-int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc* d) {
-  const int rc = check_kv(p, s, &d->kv);
-  if (rc != CLAIM_OK) return rc;
-  if (d->reserved != 0 || (p.dim != 64 && p.dim != 128) || p.chunk_bytes > 0xFFFFFFFFull)
-    return CLAIM_EINVAL;
-  if (d->num_heads == 0 || d->num_heads % p.heads || d->num_heads / p.heads > 64) return CLAIM_EINVAL;
-  if (!finite_positive(d->scale)) return CLAIM_EINVAL;
-  if ((uint64_t)d->prefix_blocks * p.bs > 0x7FFFFFFFull || (d->prefix_blocks && !d->prefix))
-    return CLAIM_EINVAL;
-  // a wave of the joining kernel for each row and query head, a workgroup of 512
-  // threads for each sequence and KV head: fewer than 2^32 threads
-  if ((uint64_t)d->kv.num_rows * d->num_heads >= 1u << 26 || (uint64_t)d->kv.num_seqs * p.heads > 1u << 22)
-    return CLAIM_EINVAL;
-  return CLAIM_OK;
-}
-
 template <int D, bool E4M3, Within WITHIN>
 void launch_few(const PoolView& p, const Plan& plan, const Args& a, uint32_t prefix, uint32_t own) {
   const dim3 both((own + 7) / 8 * 8 + (prefix + 7) / 8 * 8);
@@ -205,39 +189,9 @@ int claim_attend(claim_pool* P, const claim_seqs* s, const claim_attend_desc* d)
   const uint64_t need = plan_bytes(plan, p.dim);
   if (need && ((uintptr_t)d->work & 255)) return CLAIM_EINVAL;
   if (need && (!d->work || d->work_bytes < need)) return CLAIM_ENOSPC;
-  SEQ_HIP(hipSetDevice(p.device));
   Args a{};
-  a.q = (const uint16_t*)d->q.data;
-  a.out = (uint16_t*)d->out.data;
-  a.q_row = d->q.row_stride;
-  a.q_head = d->q.head_stride;
-  a.out_row = d->out.row_stride;
-  a.out_head = d->out.head_stride;
-  a.rows = d->kv.num_rows;
-  a.num_seqs = d->kv.num_seqs;
-  a.group = d->num_heads / p.heads;
-  a.heads = p.heads;
-  a.ids = d->kv.ids;
-  a.offsets = d->kv.offsets;
-  a.max_seqs = s->max_seqs;
-  a.max_blocks = s->max_blocks;
-  a.tables = s->tables;
-  a.lengths = s->lengths;
-  a.prefix = d->prefix;
-  a.prefix_tokens = d->prefix_blocks * p.bs;
-  a.bs = p.bs;
-  a.bs_magic = 0xFFFFFFFFu / p.bs;
-  a.nb = p.nb;
-  a.chunk_bytes = (uint32_t)p.chunk_bytes;
-  a.token_bytes = p.heads * p.dim * p.elem;
-  const uint64_t plane = (uint64_t)p.nb * p.chunk_bytes;
-  a.k = p.kv + 2ull * d->kv.layer * plane;
-  a.v = a.k + plane;
-  const float log2e = 1.44269504088896340736f;
-  a.c = d->scale * d->kv.k_scale * log2e;
-  if (!finite_positive(a.c)) return CLAIM_EINVAL;
-  a.margin = 8.0f / a.c;
-  a.v_scale = d->kv.v_scale;
+  if (!fill_args(p, s, d, &a)) return CLAIM_EINVAL;
+  SEQ_HIP(hipSetDevice(p.device));
   a.own_splits = plan.own_splits;
   a.prefix_splits = plan.prefix_splits;
   a.tiles = plan.tiles;

@@ -71,6 +71,36 @@ struct Args {
   float2* part_ml;  // [row][query head][split]: maximum, sum
 };
 
+// With windows, a row at position P sees P - window + 1 .. P and the first `sinks`.
+struct WindowArgs : Args {
+  uint32_t window, sinks;
+  uint32_t room;    // positions that a table has: a row at one of them or later sees it
+  float* part_sum;  // [row][query head][split]: the sum of the weights before rounding
+  float* lse;       // [row][query head], or none
+};
+
+template <bool WIN>
+using ArgsOf = std::conditional_t<WIN, WindowArgs, Args>;
+
+// Which keys of a tile a row sees: the first `hi`, and with a window those of them
+// from `lo` on or before `few`.
+template <bool WIN>
+struct Seen {
+  int hi;
+  __device__ __forceinline__ bool key(int x, int from = 0) const { return x < hi - from; }
+  __device__ __forceinline__ bool all(int keys) const { return !(hi < keys); }
+};
+
+template <>
+struct Seen<true> {
+  int hi, lo, few;
+  __device__ __forceinline__ bool key(int x, int from = 0) const {
+    return x < hi - from && (x >= lo - from || x < few - from);
+  }
+  __device__ __forceinline__ bool all(int keys) const { return hi >= keys && (lo <= 0 || few >= keys); }
+  __device__ __forceinline__ bool any() const { return hi > lo || (hi > 0 && few > 0); }
+};
+
 // A query row of this lane.
 struct Row {
   bool valid;
@@ -81,6 +111,15 @@ struct Row {
 // What the row's results are divided by turns into: 0 for a row that sees nothing.
 // One that sees keys of score -infinity alone has 0 / 0, as its formula does.
 __device__ __forceinline__ float over_sum(float x, float sum, bool sees) { return sees ? x / sum : 0.0f; }
+
+// The logarithm of a row's sum of exponentials: -infinity for one that sees
+// nothing, or scores of -infinity alone.
+__device__ __forceinline__ void write_lse(const WindowArgs& a, uint32_t row, uint32_t head, float m, float sum) {
+  if (!a.lse) return;
+  constexpr float kLn2 = 0.693147180559945309f;
+  const float x = sum == 0.0f ? kNoMax : __builtin_fmaf(m, a.c, log2f(sum)) * kLn2;
+  a.lse[(uint64_t)row * a.heads * a.group + head] = x;
+}
 
 // A value that all lanes of the wave have, for the scalar unit.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -97,6 +136,67 @@ struct Range {
   uint32_t entries;
   uint32_t lo, hi;
 };
+
+// The groups of KEYS keys that a tile of rows with windows reads, each aligned to
+// its size: n0 from position f0 on, of which all rows see the first `full` whole,
+// then n1 from b0 on, where windows begin, then the first ones of the sequence.
+// What is seen by all comes first, as the order of keys does not matter to a sum.
+struct Walk {
+  uint32_t f0, n0, b0, n1, full;
+  uint32_t from, count;  // this split's groups
+  uint32_t end;          // positions from here on are not read
+};
+
+template <uint32_t KEYS>
+__device__ __forceinline__ uint32_t walk_pos(const Walk& w, uint32_t n) {
+  const uint32_t x = w.from + n;
+  return x < w.n0 ? w.f0 + x * KEYS : x < w.n0 + w.n1 ? w.b0 + (x - w.n0) * KEYS : (x - w.n0 - w.n1) * KEYS;
+}
+
+// Rows at positions first .. last of a sequence, each with its window and the first
+// keys; `last` < 0: nothing is seen.  Of positions past the table, the first is read
+// by all rows that have come so far: a wrong length cannot hold the GPU.
+template <uint32_t KEYS>
+__device__ __forceinline__ Walk make_walk(const WindowArgs& a, int64_t first, int64_t last, uint32_t split,
+                                          uint32_t splits) {
+  Walk w;
+  w.end = last < 0 ? 0 : last < (int64_t)a.room ? (uint32_t)(last + 1) : a.room + 1;
+  const auto begins = [&](int64_t p) { return p + 1 - a.window < (int64_t)a.room ? p + 1 - a.window : a.room; };
+  const int64_t low = begins(first), high = begins(last);  // where windows begin
+  const uint32_t few = a.sinks < w.end ? a.sinks : w.end;
+  uint32_t n2 = (few + KEYS - 1) / KEYS;  // groups of the first keys
+  const uint32_t begin = low > 0 ? (uint32_t)low / KEYS : 0;
+  const uint32_t groups = w.end / KEYS + (w.end % KEYS != 0);
+  uint32_t b = begin > n2 ? begin : n2;
+  b = b < groups ? b : groups;
+  n2 = n2 < b ? n2 : b;
+  // from `f` on, all rows' windows have begun; below `t`, none has ended
+  uint32_t f = high > 0 ? (uint32_t)(high / KEYS + (high % KEYS != 0)) : 0;
+  const int64_t least = first + 1 < (int64_t)w.end ? first + 1 : w.end;
+  const uint32_t t = least > 0 ? (uint32_t)(least / KEYS) : 0;
+  f = f > b ? f : b;
+  if (f >= t) f = b;
+  w.full = f < t && high <= (int64_t)f * KEYS ? t - f : 0;
+  w.f0 = f * KEYS;
+  w.n0 = groups - f;
+  w.b0 = b * KEYS;
+  w.n1 = f - b;
+  const uint32_t all = w.n0 + w.n1 + n2;
+  uint32_t share = (all + splits - 1) / splits;
+  w.from = share * split < all ? share * split : all;
+  w.count = all - w.from < share ? all - w.from : share;
+  w.full = w.full > w.from ? w.full - w.from : 0;
+  w.full = w.full < w.count ? w.full : w.count;
+  w.f0 = uniform(w.f0);
+  w.n0 = uniform(w.n0);
+  w.b0 = uniform(w.b0);
+  w.n1 = uniform(w.n1);
+  w.full = uniform(w.full);
+  w.from = uniform(w.from);
+  w.count = uniform(w.count);
+  w.end = uniform(w.end);
+  return w;
+}
 
 __device__ __forceinline__ void split_pos(const Args& a, uint32_t pos, uint32_t* block,
                                           uint32_t* token) {
@@ -431,15 +531,15 @@ struct Wave {
       }
   }
 
-  // Takes out the keys past the first `seen` of the tile.
-  template <int U>
-  __device__ __forceinline__ void mask(f32x16 (&s)[U], int seen) const {
+  // Takes out the keys of the tile that the row does not see.
+  template <int U, bool WIN>
+  __device__ __forceinline__ void mask(f32x16 (&s)[U], const Seen<WIN>& seen) const {
     const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        s[u][r] = 32 * u + 8 * (r / 4) + r % 4 < seen - 4 * h ? s[u][r] : kNoMax;
+        s[u][r] = seen.key(32 * u + 8 * (r / 4) + r % 4, 4 * h) ? s[u][r] : kNoMax;
   }
 
   // Weights of a tile, and the running maximum and sum.
@@ -511,13 +611,14 @@ struct Wave {
     __builtin_amdgcn_sched_group_barrier(kMul, 4, 0);
   }
 
-  // A whole tile of which the lane's row sees the first `seen` keys.
-  template <int U>
-  __device__ __forceinline__ void tile(const Args& a, const uint8_t* lk, const uint8_t* lv, int seen) {
+  // A whole tile of which the lane's row sees the keys `seen`.
+  template <int U, bool WIN>
+  __device__ __forceinline__ void tile(const Args& a, const uint8_t* lk, const uint8_t* lv,
+                                       const Seen<WIN>& seen) {
     f32x16 s[U];
     bf16x8 p[U][2];
     scores<U>(lk, s);
-    const bool masked = __any(seen < 32 * U);
+    const bool masked = __any(!seen.all(32 * U));
     if (masked) mask<U>(s, seen);
     weights<U>(a, s, p);
     if (masked && nonfinite<U>(lv))
@@ -543,8 +644,9 @@ struct Wave {
 
   // values() where V holds infinities or NaN that some rows do not see: one
   // key's product at a time, kept by the rows that see the key.
-  template <int U>
-  __device__ __forceinline__ void values_seen(const uint8_t* lv, const bf16x8 (&p)[U][2], int seen) {
+  template <int U, bool WIN>
+  __device__ __forceinline__ void values_seen(const uint8_t* lv, const bf16x8 (&p)[U][2],
+                                              const Seen<WIN>& seen) {
     const uint32_t at = lds_address(lv) + v_lane, h = (threadIdx.x >> 5) & 1;
 #pragma unroll 1
     for (uint32_t key = 0; key < 32 * U; ++key) {
@@ -563,19 +665,22 @@ struct Wave {
         const u32x4 v = __builtin_bit_cast(u32x4, v_operand(at + key / 16 * 16 * D * 2, 0, 0, j)) & only;
         const f32x16 with = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), weight, o[j], 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[j][r] = (int)key < seen ? with[r] : o[j][r];
+        for (int r = 0; r < 16; ++r) o[j][r] = seen.key((int)key) ? with[r] : o[j][r];
       }
     }
   }
 
   // The rows' parts for the joining kernel: through LDS of the wave's own (32
   // rows of D floats), so that whole rows are stored at a time.
-  __device__ __forceinline__ void finish_part(const Args& a, const Row& r, bool sees, uint32_t split,
+  template <bool WIN>
+  __device__ __forceinline__ void finish_part(const ArgsOf<WIN>& a, const Row& r, bool sees, uint32_t split,
                                               uint32_t splits, uint8_t* lds) {
     const uint32_t lane = threadIdx.x & 63, h = lane >> 5, row = lane & 31;
     const float sum = across_halves_add(l);
     uint64_t at = ((uint64_t)r.row * a.heads * a.group + r.head) * splits + split;
     if (r.valid && h == 0) a.part_ml[at] = float2{sees ? fmaxf(m, kLeast) : m, sum};
+    if constexpr (WIN)
+      if (r.valid && h == 0) a.part_sum[at] = sum;
     if (!r.valid || sum == 0.0f) at = ~0ull;
     constexpr uint32_t kChunks = D / 4;  // 16-byte chunks of a row, exchanged by its number
 #pragma unroll
@@ -597,10 +702,13 @@ struct Wave {
   }
 
   // The rows' results.
-  __device__ __forceinline__ void finish(const Args& a, const Row& r, bool sees) {
+  template <bool WIN>
+  __device__ __forceinline__ void finish(const ArgsOf<WIN>& a, const Row& r, bool sees) {
     const uint32_t h = (threadIdx.x >> 5) & 1;
     const float sum = across_halves_add(l);
     if (!r.valid) return;
+    if constexpr (WIN)
+      if (h == 0) write_lse(a, r.row, r.head, m, sum);
     const float f = over_sum(a.v_scale, sum, sees);
     uint16_t* dst = a.out + r.row * a.out_row + r.head * a.out_head + 4 * h;
 #pragma unroll
@@ -627,6 +735,7 @@ struct Tile {
   int64_t len;         // own: the sequence's tokens
   uint32_t kv_head;
   Range range;
+  Walk walk;  // with windows, in place of the range's positions
 };
 
 // The last sequence whose tiles start at or before `tile`.  Sequence s starts
@@ -699,8 +808,8 @@ __device__ __forceinline__ Ordered ordered_tile(const Args& a, uint32_t place) {
 }
 
 // ORDERED: `tile` is a place in the order above where there is one.
-template <int M, bool ORDERED>
-__device__ __forceinline__ Tile make_tile(const Args& a, bool prefix, uint32_t tile, uint32_t split,
+template <int M, bool ORDERED, uint32_t KEYS, bool WIN>
+__device__ __forceinline__ Tile make_tile(const ArgsOf<WIN>& a, bool prefix, uint32_t tile, uint32_t split,
                                           uint32_t splits, uint32_t kv_head, uint32_t align) {
   Tile it;
   it.prefix = prefix;
@@ -759,6 +868,13 @@ __device__ __forceinline__ Tile make_tile(const Args& a, bool prefix, uint32_t t
     lo = a.prefix_tokens;
     const uint32_t last = it.x0 + M < it.all ? it.x0 + M : it.all;
     top = it.any ? it.len - it.n + (last + a.group - 1) / a.group : 0;
+  }
+  if constexpr (WIN) {
+    const int64_t first = it.any ? it.len - it.n + it.x0 / a.group : -1;
+    it.walk = make_walk<KEYS>(a, first, top - 1, split, splits);
+    it.range.list = uniform(it.range.list);
+    it.range.entries = uniform(it.range.entries);
+    return it;
   }
   // a row that sees a position past the table is NaN whatever else it sees:
   // one such position is enough, and a wrong length cannot hold the GPU
@@ -845,9 +961,18 @@ __device__ __forceinline__ void hold(bf16x8 (&p)[2][2]) {
   }
 }
 
-// How many of the `keys` positions from `pos` on the row sees.
-__device__ __forceinline__ int seen_of(const Row& r, uint32_t pos, uint32_t keys) {
-  return r.limit <= pos ? 0 : r.limit - pos < keys ? (int)(r.limit - pos) : (int)keys;
+// Which of the `keys` positions from `pos` on the row sees.
+template <bool WIN>
+__device__ __forceinline__ Seen<WIN> seen_of(const ArgsOf<WIN>& a, const Row& r, uint32_t pos, uint32_t keys) {
+  const auto upto = [&](uint32_t end) { return end <= pos ? 0 : end - pos < keys ? (int)(end - pos) : (int)keys; };
+  Seen<WIN> s;
+  s.hi = upto(r.limit);
+  if constexpr (WIN) {
+    const uint32_t low = r.limit > a.window ? r.limit - a.window : 0;
+    s.lo = upto(low < a.room ? low : a.room);
+    s.few = upto(a.sinks);
+  }
+  return s;
 }
 
 // ----------------------------------------------------------- many query rows
@@ -885,8 +1010,8 @@ struct Many {
   };
 };
 
-template <int D, bool E4M3, int WAVES, Within WITHIN>
-__device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b,
+template <int D, bool E4M3, int WAVES, Within WITHIN, bool WIN = false>
+__device__ __forceinline__ void many_rows(const ArgsOf<WIN>& a, bool prefix, uint32_t b,
                                           typename Many<D, WAVES>::Lds& shared) {
   using F = Many<D, WAVES>;
   constexpr int M = WAVES * 32, kKeys = F::kKeys, kTile = F::kTile, kAhead = F::kAhead;
@@ -898,7 +1023,7 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
   b /= a.heads;
   const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
   const uint32_t split = b % splits;
-  const Tile it = make_tile<M, true>(a, prefix, b / splits, split, splits, kv_head, kKeys);
+  const Tile it = make_tile<M, true, kKeys, WIN>(a, prefix, b / splits, split, splits, kv_head, kKeys);
   if (!it.any) return;
   const uint64_t head_bytes = (uint64_t)kv_head * D * (E4M3 ? 1 : 2);
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
@@ -909,20 +1034,30 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
   typename St::Places kp, vp;
   const uint32_t add_blocks = kKeys / a.bs, add_tokens = kKeys % a.bs;
   const auto left = [&](uint32_t tile) {  // rows of the tile that the range has
+    if constexpr (WIN) {
+      const uint32_t from = walk_pos<kKeys>(it.walk, tile);
+      return tile < it.walk.count && from < it.walk.end ? it.walk.end - from : 0;
+    }
     const uint32_t from = lo + tile * kKeys;
     return from < hi ? hi - from : 0;
+  };
+  const auto next = [&](uint32_t tile, typename St::Rows& r) {  // of tile `tile`, after the one before it
+    if (WIN)
+      st.first(a, walk_pos<kKeys>(it.walk, tile), r);
+    else
+      st.next(a, add_blocks, add_tokens, r);
   };
   // copies begin before anything else: tiles 0 and 1 of K and 0 of V, then
   // what W(-1) would have asked for, 2 of K and 1 of V
   {
     typename St::Rows ahead[kAhead];
     typename St::Held first[2];
-    st.first(a, lo, rows);
+    st.first(a, WIN ? walk_pos<kKeys>(it.walk, 0) : lo, rows);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       ahead[i] = rows;
       st.look(it.range, ahead[i]);
-      st.next(a, add_blocks, add_tokens, rows);
+      next(i + 1, rows);
     }
     st.look(it.range, rows);
     vp = st.place(a, ahead[0], left(0));
@@ -941,16 +1076,22 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
   const Row row = row_at(a, it, (t >> 6) * 32 + (t & 31));
   Wave<D> w;
   w.start(a, row);
-  uint32_t wave_hi, wave_least;
-  seen_by_wave(row, 32, &wave_hi, &wave_least);
-  // whole tiles that every row of the workgroup sees
-  if ((t & 63) == 0) least[t >> 6] = wave_least;
-  wait_loads();
-  meet();
-  uint32_t below = hi;
+  uint32_t wave_hi, wave_least, full;
+  if constexpr (WIN) {
+    wait_loads();
+    meet();
+    full = it.walk.full;
+  } else {
+    seen_by_wave(row, 32, &wave_hi, &wave_least);
+    // whole tiles that every row of the workgroup sees
+    if ((t & 63) == 0) least[t >> 6] = wave_least;
+    wait_loads();
+    meet();
+    uint32_t below = hi;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) below = least[i] < below ? least[i] : below;
-  const uint32_t full = uniform(below > lo ? (below - lo) / kKeys : 0);
+    for (int i = 0; i < WAVES; ++i) below = least[i] < below ? least[i] : below;
+    full = uniform(below > lo ? (below - lo) / kKeys : 0);
+  }
 
   uint32_t now = 0, n = 0;  // tile n is at `now` in the ring
   const auto before = [&](uint32_t x) { return x ? x - kTile : kAhead * kTile; };
@@ -964,7 +1105,7 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
     kp = st.place(a, rows, left(n + kAhead));
     st.template issue<true>(k, kp, lk + to, kh);
     st.template issue<false>(v, vp, lv + before(to), vh);
-    st.next(a, add_blocks, add_tokens, rows);
+    next(n + kAhead + 1, rows);
     st.look(it.range, rows);
   };
   const auto step = [&] {
@@ -1000,26 +1141,41 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
     if (uniform(t >> 6) < WAVES / 2) meet();
     meet();
   }
+  if constexpr (WIN) {
 #pragma unroll 1
-  for (uint32_t pos = lo + full * kKeys; pos < hi; pos += kKeys) {  // hi + kKeys fits 32 bits
-    const bool more = pos + kKeys < hi;
-    if (more) fetch();
-    if (pos < wave_hi) w.template tile<2>(a, lk + now, lv + now, seen_of(row, pos, kKeys));
-    if (!more) break;
-    step();
-    wait_loads();
-    meet();
+    for (; n < it.walk.count;) {
+      const bool more = n + 1 < it.walk.count;
+      if (more) fetch();
+      const auto seen = seen_of<true>(a, row, walk_pos<kKeys>(it.walk, n), kKeys);
+      if (__any(seen.any())) w.template tile<2, true>(a, lk + now, lv + now, seen);
+      if (!more) break;
+      step();
+      wait_loads();
+      meet();
+    }
+  } else {
+#pragma unroll 1
+    for (uint32_t pos = lo + full * kKeys; pos < hi; pos += kKeys) {  // hi + kKeys fits 32 bits
+      const bool more = pos + kKeys < hi;
+      if (more) fetch();
+      if (pos < wave_hi) w.template tile<2, false>(a, lk + now, lv + now, seen_of<false>(a, row, pos, kKeys));
+      if (!more) break;
+      step();
+      wait_loads();
+      meet();
+    }
   }
-  const bool sees = row.limit > lo && hi > lo;
+  // with a window, a split's part counts as seen where the row sees any key at all
+  const bool sees = WIN ? row.limit > 0 : row.limit > lo && hi > lo;
   if (a.part_o) {
     meet();  // the tiles have been read
     constexpr uint32_t kRoom = 32 * D * 4;
     static_assert(WAVES / 2 * kRoom <= 4 * kTile, "");
     const uint32_t wave = uniform(t >> 6);
-    w.finish_part(a, row, sees, prefix ? a.own_splits + split : split, a.own_splits + a.prefix_splits,
+    w.template finish_part<WIN>(a, row, sees, prefix ? a.own_splits + split : split, a.own_splits + a.prefix_splits,
                   wave < WAVES / 2 ? lk + wave * kRoom : lv + (wave - WAVES / 2) * kRoom);
   } else {
-    w.finish(a, row, sees);
+    w.template finish<WIN>(a, row, sees);
   }
 }
 
@@ -1043,13 +1199,14 @@ __device__ __forceinline__ void many_rows(const Args& a, bool prefix, uint32_t b
 // each 16, which is P^T's operand of a 16 x 16 x 16 product, and of a 16 x 16 x
 // 32 one over two groups of 16 if V^T's operand takes its keys in that order.
 
-template <int D, bool E4M3, int QT, int KEYS>
+template <int D, bool E4M3, int QT, int KEYS, bool WIN>
 struct Narrow {
   static constexpr int kBytes = D * (E4M3 ? 1 : 2), kSub = KEYS / 16;
   static_assert(KEYS == 32 || (KEYS == 16 && !E4M3), "");
   bf16x8 q[QT][D / 32];
   f32x4 o[QT][D / 16];
   float m[QT], l[QT];  // the maximum is the row's; the sum this lane's share
+  float e[WIN ? QT : 1];  // the sum before rounding, for its logarithm
   uint32_t k_lane, v_lane;
 
   __device__ __forceinline__ void start(const Args& a, const Row (&row)[QT]) {
@@ -1067,6 +1224,7 @@ struct Narrow {
       for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{};
       m[c] = kNoMax;
       l[c] = 0;
+      if (WIN) e[c] = 0;
     }
     using S = NarrowSwizzle<kBytes>;
     if (E4M3) {
@@ -1108,7 +1266,7 @@ struct Narrow {
 
   // Weights of a group, and the running maximum and sum (see Wave::weights).
   __device__ __forceinline__ void weights(const Args& a, f32x4 (&s)[QT][kSub], bool masked,
-                                          const int (&seen)[QT]) {
+                                          const Seen<WIN> (&seen)[QT]) {
     const int g4 = ((threadIdx.x >> 4) & 3) * 4;
     float top[QT];
     bool up = false;
@@ -1119,7 +1277,7 @@ struct Narrow {
       for (int n = 0; n < kSub; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          if (masked) s[c][n][r] = 16 * n + r < seen[c] - g4 ? s[c][n][r] : kNoMax;
+          if (masked) s[c][n][r] = seen[c].key(16 * n + r, g4) ? s[c][n][r] : kNoMax;
           x = fmaxf(x, s[c][n][r]);
         }
       const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -1132,6 +1290,7 @@ struct Narrow {
         const float to = fmaxf(m[c], top[c]), base = to == kNoMax ? 0.0f : to;
         const float f = __builtin_amdgcn_exp2f((m[c] - base) * a.c);
         l[c] *= f;
+        if (WIN) e[c] *= f;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) o[c][j] *= f;
         m[c] = to;
@@ -1146,7 +1305,9 @@ struct Narrow {
         for (int r = 0; r < 4; ++r) {
           // the weight that is summed is the rounded one that multiplies V:
           // what rounding does to a row's heaviest weights divides out again
-          s[c][n][r] = (float)(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], a.c, -mc));
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], a.c, -mc));
+          if (WIN) e[c] += x;
+          s[c][n][r] = (float)(__bf16)x;
           l[c] += s[c][n][r];
         }
     }
@@ -1193,7 +1354,7 @@ struct Narrow {
   }
 
   __device__ __forceinline__ void values(const uint8_t* lv, const f32x4 (&s)[QT][kSub], bool masked,
-                                         const int (&seen)[QT]) {
+                                         const Seen<WIN> (&seen)[QT]) {
     uint32_t at = lds_address(lv) + v_lane;
     asm volatile("" : "+v"(at));
     if (masked && nonfinite(lv)) {
@@ -1232,7 +1393,8 @@ struct Narrow {
 
   // values() where V holds infinities or NaN that some rows do not see: one
   // key's product at a time, kept by the rows that see the key.
-  __device__ __forceinline__ void values_seen(uint32_t at, const f32x4 (&s)[QT][kSub], const int (&seen)[QT]) {
+  __device__ __forceinline__ void values_seen(uint32_t at, const f32x4 (&s)[QT][kSub],
+                                              const Seen<WIN> (&seen)[QT]) {
     const uint32_t g = (threadIdx.x >> 4) & 3;
     constexpr int kWords = KEYS / 8;
     typedef uint32_t words __attribute__((ext_vector_type(kWords)));
@@ -1254,7 +1416,7 @@ struct Narrow {
           const V v = __builtin_bit_cast(V, __builtin_bit_cast(words, v_operand(at, j)) & only);
           const f32x4 with = multiply(v, weight, o[c][j]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[c][j][r] = (int)key < seen[c] ? with[r] : o[c][j][r];
+          for (int r = 0; r < 4; ++r) o[c][j][r] = seen[c].key((int)key) ? with[r] : o[c][j][r];
         }
       }
     }
@@ -1272,11 +1434,15 @@ struct Few {
     __align__(1024) uint8_t ring[kRing];
     float tops[kWaves][kRows], sums[kWaves][kRows];
   };
+  struct WithSums : Lds {
+    float exact[kWaves][kRows];
+  };
 };
 
-template <int D, bool E4M3, int WAVES, Within WITHIN, int QT>
-__device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
-                                         typename Few<D, E4M3, WAVES>::Lds& shared) {
+template <int D, bool E4M3, int WAVES, Within WITHIN, int QT, bool WIN = false>
+__device__ __forceinline__ void few_rows(
+    const ArgsOf<WIN>& a, bool prefix, uint32_t b,
+    std::conditional_t<WIN, typename Few<D, E4M3, WAVES>::WithSums, typename Few<D, E4M3, WAVES>::Lds>& shared) {
   using F = Few<D, E4M3, WAVES>;
   constexpr int M = 16 * QT, kKeys = F::kKeys, kTile = F::kTile, kWaves = F::kWaves;
   using St = Stage<F::kBytes, false, kKeys, 64, WITHIN, NarrowSwizzle<F::kBytes>>;
@@ -1288,38 +1454,52 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
   b /= a.heads;
   const uint32_t splits = prefix ? a.prefix_splits : a.own_splits;
   const uint32_t split = b % splits, tile = b / splits;
-  const Tile it = make_tile<M, false>(a, prefix, tile, split, splits, kv_head, kKeys);
+  const Tile it = make_tile<M, false, kKeys, WIN>(a, prefix, tile, split, splits, kv_head, kKeys);
   if (!it.any) return;
   const uint64_t head_bytes = (uint64_t)kv_head * F::kBytes;
   const uint8_t *k = a.k + head_bytes, *v = a.v + head_bytes;
   // groups wave, wave + 4, ... of the range
   constexpr uint32_t kStep = kWaves * kKeys;
-  const uint32_t hi = it.range.hi;
-  uint32_t pos = it.range.lo + wave * kKeys;
+  // (with windows, `pos` and `hi` count groups, and a step is one for each wave)
+  const uint32_t hi = WIN ? it.walk.count : it.range.hi;
+  uint32_t pos = WIN ? wave : it.range.lo + wave * kKeys;
+  constexpr uint32_t kMore = WIN ? kWaves : kStep;
   uint8_t* const lk = lds + wave * 4 * kTile;
   uint8_t* const lv = lk + 2 * kTile;
-  Narrow<D, E4M3, QT, kKeys> w;
+  Narrow<D, E4M3, QT, kKeys, WIN> w;
   const St st(a, t);
   const uint32_t add_blocks = kStep / a.bs, add_tokens = kStep % a.bs;
-  const auto rest = [&](uint32_t from) { return from < hi ? hi - from : 0; };
+  const auto rest = [&](uint32_t from) {
+    if constexpr (WIN) {
+      const uint32_t x = walk_pos<kKeys>(it.walk, from);
+      return from < hi && x < it.walk.end ? it.walk.end - x : 0;
+    }
+    return from < hi ? hi - from : 0;
+  };
+  const auto next = [&](uint32_t to, typename St::Rows& r) {
+    if (WIN)
+      st.first(a, walk_pos<kKeys>(it.walk, to), r);
+    else
+      st.next(a, add_blocks, add_tokens, r);
+  };
   typename St::Rows rows;
   typename St::Places at;
   typename St::Held none;
   if (pos < hi) {  // copies begin before anything else
     typename St::Rows second;
-    st.first(a, pos, rows);
+    st.first(a, WIN ? walk_pos<kKeys>(it.walk, pos) : pos, rows);
     second = rows;
-    st.next(a, add_blocks, add_tokens, second);
+    next(pos + kMore, second);
     st.look(it.range, rows);
     st.look(it.range, second);
-    at = st.place(a, rows, hi - pos);
+    at = st.place(a, rows, WIN ? rest(pos) : hi - pos);
     st.template issue<true>(k, at, lk, none);
     st.template issue<false>(v, at, lv, none);
-    at = st.place(a, second, rest(pos + kStep));
+    at = st.place(a, second, rest(pos + kMore));
     st.template issue<true>(k, at, lk + kTile, none);
     st.template issue<false>(v, at, lv + kTile, none);
     rows = second;
-    st.next(a, add_blocks, add_tokens, rows);
+    next(pos + 2 * kMore, rows);
     st.look(it.range, rows);
   }
   Row row[QT];
@@ -1337,10 +1517,13 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
     constexpr int kLater = 3 * St::kSteps;  // copies begun after the one that is waited for
     const auto group = [&](auto masked) {
       f32x4 s[QT][kKeys / 16];
-      int seen[QT];
+      Seen<WIN> seen[QT];
 #pragma unroll
-      for (int c = 0; c < QT; ++c) seen[c] = masked ? seen_of(row[c], pos, kKeys) : kKeys;
-      at = st.place(a, rows, rest(pos + 2 * kStep));
+      for (int c = 0; c < QT; ++c) {
+        seen[c] = {kKeys};
+        if (masked) seen[c] = seen_of<WIN>(a, row[c], WIN ? walk_pos<kKeys>(it.walk, pos) : pos, kKeys);
+      }
+      at = st.place(a, rows, rest(pos + 2 * kMore));
       wait_copies<kLater>();
       w.scores(lk + x, s);
       wait_lds();
@@ -1351,17 +1534,17 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
       // table entries are read where the products of V hide it: scalar loads
       // and LDS reads share a counter
       __builtin_amdgcn_sched_barrier(0);
-      st.next(a, add_blocks, add_tokens, rows);
+      next(pos + 3 * kMore, rows);
       st.look(it.range, rows);
       wait_lds();
       st.template issue<false>(v, at, lv + x, none);
     };
     // groups that all rows see, then the others; hi + 2 kStep fits 32 bits
-    const uint32_t whole = least < hi ? least : hi;
+    const uint32_t whole = WIN ? it.walk.full : least < hi ? least : hi;
 #pragma unroll 1
-    for (; pos + kKeys <= whole; pos += kStep, x ^= kTile) group(std::false_type{});
+    for (; WIN ? pos < whole : pos + kKeys <= whole; pos += kMore, x ^= kTile) group(std::false_type{});
 #pragma unroll 1
-    for (; pos < hi; pos += kStep, x ^= kTile) group(std::true_type{});
+    for (; pos < hi; pos += kMore, x ^= kTile) group(std::true_type{});
     wait_loads();
   }
   // join the waves: each row's common maximum first, then two and two
@@ -1370,6 +1553,10 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
     if (t < 16) tops[wave][16 * c + t] = w.m[c];
     w.l[c] += __shfl_xor(w.l[c], 16);
     w.l[c] += __shfl_xor(w.l[c], 32);
+    if (WIN) {
+      w.e[c] += __shfl_xor(w.e[c], 16);
+      w.e[c] += __shfl_xor(w.e[c], 32);
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -1380,6 +1567,8 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
     const float f = w.m[c] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f((w.m[c] - m) * a.c);
     w.m[c] = m;
     if (t < 16) sums[wave][16 * c + t] = w.l[c] * f;  // a wave that saw nothing adds zeros
+    if constexpr (WIN)
+      if (t < 16) shared.exact[wave][16 * c + t] = w.e[c] * f;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) w.o[c][j] *= f;
   }
@@ -1412,15 +1601,23 @@ __device__ __forceinline__ void few_rows(const Args& a, bool prefix, uint32_t b,
     w.l[c] = 0;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) w.l[c] += sums[i][16 * c + (t & 15)];
-    const bool sees = row[c].limit > it.range.lo && hi > it.range.lo;
+    const bool sees = WIN ? row[c].limit > 0 : row[c].limit > it.range.lo && hi > it.range.lo;
+    float exact = 0;
+    if constexpr (WIN)
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) exact += shared.exact[i][16 * c + (t & 15)];
     if (a.part_o) {
       const uint64_t to = ((uint64_t)row[c].row * a.heads * a.group + row[c].head) * all +
                           (prefix ? a.own_splits + split : split);
       if (t < 16) a.part_ml[to] = float2{sees ? fmaxf(w.m[c], kLeast) : w.m[c], w.l[c]};
+      if constexpr (WIN)
+        if (t < 16) a.part_sum[to] = exact;
       if (w.l[c] == 0.0f) continue;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) *(f32x4*)(a.part_o + to * D + 16 * j + g4) = w.o[c][j];
     } else {
+      if constexpr (WIN)
+        if (t < 16) write_lse(a, row[c].row, row[c].head, w.m[c], exact);
       const float f = over_sum(a.v_scale, w.l[c], sees);
       uint16_t* dst = a.out + row[c].row * a.out_row + row[c].head * a.out_head + g4;
 #pragma unroll
@@ -1443,8 +1640,8 @@ constexpr uint32_t kMostSplits = 64;  // of either kind: two parts to a lane of 
 // bytes a lane, 64 / (D / 4) parts at a time, four such loads in flight.  Bound by
 // memory and by its beginning: 17 parts of 64 rows and 32 heads of 128, 17.9 MB,
 // take 6.0 us.
-template <int D>
-__global__ void __launch_bounds__(256) k_join(Args a) {
+template <int D, bool WIN = false>
+__global__ void __launch_bounds__(256) k_join(ArgsOf<WIN> a) {
   constexpr uint32_t kLanes = D / 4, kSide = 64 / kLanes;
   const uint32_t heads = a.heads * a.group, splits = a.own_splits + a.prefix_splits;
   const uint32_t x = blockIdx.x * 4 + uniform(threadIdx.x >> 6);
@@ -1467,6 +1664,18 @@ __global__ void __launch_bounds__(256) k_join(Args a) {
   }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+  if constexpr (WIN) {
+    if (a.lse) {
+      float sum = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (f[i] >= 0) sum += a.part_sum[(uint64_t)x * splits + lane + 64 * i] * f[i];
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+      if (l != l) sum = l;  // the part of a NaN has no factor
+      if (lane == 0) write_lse(a, x / heads, x % heads, m, sum);
+    }
+  }
   const float* src = a.part_o + (uint64_t)x * splits * D + lane % kLanes * 4;
   f32x4 o = {};
   for (uint32_t s0 = 0; s0 < splits; s0 += 4 * kSide) {
@@ -1509,6 +1718,58 @@ uint32_t splits_for(uint64_t groups, uint64_t slots, uint64_t keys, uint64_t lea
 
 // Whether the rows of one load instruction of a wave lie in one block (see Stage).
 bool one_block_loads(const PoolView& p) { return p.bs % (1024 / (p.dim * p.elem)) == 0; }
+
+int check_attend(const PoolView& p, const claim_seqs* s, const claim_attend_desc* d) {
+  const int rc = check_kv(p, s, &d->kv);
+  if (rc != CLAIM_OK) return rc;
+  if (d->reserved != 0 || (p.dim != 64 && p.dim != 128) || p.chunk_bytes > 0xFFFFFFFFull)
+    return CLAIM_EINVAL;
+  if (d->num_heads == 0 || d->num_heads % p.heads || d->num_heads / p.heads > 64) return CLAIM_EINVAL;
+  if (!finite_positive(d->scale)) return CLAIM_EINVAL;
+  if ((uint64_t)d->prefix_blocks * p.bs > 0x7FFFFFFFull || (d->prefix_blocks && !d->prefix))
+    return CLAIM_EINVAL;
+  // a wave of the joining kernel for each row and query head, a workgroup of 512
+  // threads for each sequence and KV head: fewer than 2^32 threads
+  if ((uint64_t)d->kv.num_rows * d->num_heads >= 1u << 26 || (uint64_t)d->kv.num_seqs * p.heads > 1u << 22)
+    return CLAIM_EINVAL;
+  return CLAIM_OK;
+}
+
+// The arguments that a description gives, but for the plan's; false where the scores'
+// factor leaves 32 bits.
+bool fill_args(const PoolView& p, const claim_seqs* s, const claim_attend_desc* d, Args* a) {
+  a->q = (const uint16_t*)d->q.data;
+  a->out = (uint16_t*)d->out.data;
+  a->q_row = d->q.row_stride;
+  a->q_head = d->q.head_stride;
+  a->out_row = d->out.row_stride;
+  a->out_head = d->out.head_stride;
+  a->rows = d->kv.num_rows;
+  a->num_seqs = d->kv.num_seqs;
+  a->group = d->num_heads / p.heads;
+  a->heads = p.heads;
+  a->ids = d->kv.ids;
+  a->offsets = d->kv.offsets;
+  a->max_seqs = s->max_seqs;
+  a->max_blocks = s->max_blocks;
+  a->tables = s->tables;
+  a->lengths = s->lengths;
+  a->prefix = d->prefix;
+  a->prefix_tokens = d->prefix_blocks * p.bs;
+  a->bs = p.bs;
+  a->bs_magic = 0xFFFFFFFFu / p.bs;
+  a->nb = p.nb;
+  a->chunk_bytes = (uint32_t)p.chunk_bytes;
+  a->token_bytes = p.heads * p.dim * p.elem;
+  const uint64_t plane = (uint64_t)p.nb * p.chunk_bytes;
+  a->k = p.kv + 2ull * d->kv.layer * plane;
+  a->v = a->k + plane;
+  const float log2e = 1.44269504088896340736f;
+  a->c = d->scale * d->kv.k_scale * log2e;
+  a->margin = 8.0f / a->c;
+  a->v_scale = d->kv.v_scale;
+  return finite_positive(a->c);
+}
 
 }  // namespace
 

@@ -14,7 +14,7 @@ import ctypes
 import struct
 
 from . import claimkv
-from .claimkv import CAttendDesc, CKvDesc, CRotateDesc, CRows, CSeqs, ENOSPC, OK, _check, _torch, lib
+from .claimkv import CAttendDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWindowDesc, ENOSPC, OK, _check, _torch, lib
 
 SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED = 0, 1, 2
 NONE = -1  # a table entry that names no block (0xFFFFFFFF in 32 bits)
@@ -25,6 +25,8 @@ _WRITE = struct.Struct("<4I2Q2f6Q")
 _ATTEND = struct.Struct("<4I2Q2f6Q2IQfI2Q")
 assert _WRITE.size == ctypes.sizeof(CKvDesc) + 2 * ctypes.sizeof(CRows)
 _ROTATE = struct.Struct("<4I2Q2f12Q2I4Q4I2QfI")
+_WINDOW = struct.Struct(_ATTEND.format + "2IQ")
+assert _WINDOW.size == ctypes.sizeof(CWindowDesc)
 assert _ATTEND.size == ctypes.sizeof(CAttendDesc)
 assert _ROTATE.size == ctypes.sizeof(CRotateDesc)
 
@@ -76,10 +78,10 @@ class Sequences:
             pool.stream.wait_stream(torch.cuda.current_stream(dev))
             self.record_stream(pool.stream)
         self._works, self._work_at, self._work_bytes = [], 0, 0
-        self._desc = ctypes.create_string_buffer(max(_ATTEND.size, _ROTATE.size))
+        self._desc = ctypes.create_string_buffer(max(_WINDOW.size, _ROTATE.size))
         self._desc_at = ctypes.addressof(self._desc)
         self._device, self._bf16, self._int32 = dev, torch.bfloat16, torch.int32
-        self._float64 = torch.float64
+        self._float32, self._float64 = torch.float32, torch.float64
         self._heads, self._dim = g.num_kv_heads, g.head_dim
         self._lib = lib()
 
@@ -209,6 +211,17 @@ class Sequences:
         where it is, and with it a captured graph, as long as this object does."""
         return self._attend(layer, q, None, 0, 0, ids, offsets, scale, k_scale, v_scale, out)
 
+    def attend_window(self, layer: int, q, window: int | None, *, sinks: int = 0, lse=None, ids=None,
+                      offsets=None, scale: float | None = None, k_scale: float = 1.0,
+                      v_scale: float = 1.0, out=None):
+        """claim_attend_window: :meth:`attend` where a row sees the last
+        ``window`` positions (its own among them; None: all) and the first
+        ``sinks``.  Table entries of other positions are not read.  With
+        ``lse`` (float32 [rows, heads]), the logarithms of the rows' sums of
+        exponentials are written there, for :meth:`weigh`."""
+        return self._attend(layer, q, None, 0, 0, ids, offsets, scale, k_scale, v_scale, out,
+                            (*self._window(window, sinks), lse))
+
     def attend_shared(self, layer: int, q, prefix, *, ids=None, offsets=None,
                       scale: float | None = None, k_scale: float = 1.0, v_scale: float = 1.0,
                       out=None):
@@ -220,8 +233,9 @@ class Sequences:
         return self._attend(layer, q, prefix, self._ints("prefix", prefix), prefix.numel(), ids,
                             offsets, scale, k_scale, v_scale, out)
 
-    def _attend(self, layer, q, prefix, prefix_at, blocks, ids, offsets, scale, k_scale, v_scale, out):
-        pool, shape = self.pool, q.shape
+    def _attend(self, layer, q, prefix, prefix_at, blocks, ids, offsets, scale, k_scale, v_scale, out,
+                window=None):
+        pool, shape, L = self.pool, q.shape, self._lib
         if len(shape) != 3:
             raise ValueError("q must be [rows, heads, head_dim]")
         heads = shape[1]
@@ -233,26 +247,35 @@ class Sequences:
         given = (*self._kv(layer, shape[0], ids, offsets), k_scale, v_scale, *rows_q,
                  *self._rows("out", out, heads), heads, blocks, prefix_at,
                  self._dim**-0.5 if scale is None else scale, 0)
-        _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
-        with pool.ordered(self, q, out, ids, offsets, prefix):
-            rc = self._lib.claim_attend(pool._h, self._seqs_ref, self._desc_at)
-            if rc == ENOSPC:  # the first call of a larger shape
-                need = ctypes.c_uint64()
-                _check(self._lib.claim_attend_work(pool._h, self._seqs_ref, self._desc_at,
-                                               ctypes.byref(need)), "claim_attend_work")
-                # the smaller ones are kept: a captured graph holds their
-                # addresses.  Each is at least twice the one before, so all of
-                # them together are less than four times what was needed
-                size = max(need.value, 2 * self._work_bytes)
-                torch = _torch()
-                with torch.cuda.stream(pool.stream):
-                    self._works.append(torch.empty(size, dtype=torch.uint8, device=self._device))
-                self._work_at, self._work_bytes = self._works[-1].data_ptr(), size
-                _ATTEND.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes)
-                rc = self._lib.claim_attend(pool._h, self._seqs_ref, self._desc_at)
-            if rc != OK:
-                _check(rc, "claim_attend")
+        lse, record, more, call, need = None, _ATTEND, (), L.claim_attend, L.claim_attend_work
+        if window is not None:
+            width, sinks, lse = window
+            more = (width, sinks, 0 if lse is None else self._row_floats("lse", lse, shape))
+            record, call, need = _WINDOW, L.claim_attend_window, L.claim_attend_window_work
+        with pool.ordered(self, q, out, ids, offsets, prefix, lse):
+            self._with_work(record, given, more, call, need)
         return out
+
+    def _with_work(self, record, given, more, call, work):
+        """``call`` with a description that ends in its scratch (and ``more``)."""
+        pool = self.pool
+        record.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes, *more)
+        rc = call(pool._h, self._seqs_ref, self._desc_at)
+        if rc == ENOSPC:  # the first call of a larger shape
+            need = ctypes.c_uint64()
+            _check(work(pool._h, self._seqs_ref, self._desc_at, ctypes.byref(need)), work.__name__)
+            # the smaller ones are kept: a captured graph holds their
+            # addresses.  Each is at least twice the one before, so all of
+            # them together are less than four times what was needed
+            size = max(need.value, 2 * self._work_bytes)
+            torch = _torch()
+            with torch.cuda.stream(pool.stream):
+                self._works.append(torch.empty(size, dtype=torch.uint8, device=self._device))
+            self._work_at, self._work_bytes = self._works[-1].data_ptr(), size
+            record.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes, *more)
+            rc = call(pool._h, self._seqs_ref, self._desc_at)
+        if rc != OK:
+            _check(rc, call.__name__)
 
     def record_stream(self, stream) -> None:
         """The sequences' own tensors are used on ``stream``."""
@@ -264,6 +287,21 @@ class Sequences:
         """The address of a contiguous int32 tensor on the pool's device."""
         if t.dtype != self._int32 or t.device != self._device or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 tensor on {self._device}")
+        return t.data_ptr()
+
+    @staticmethod
+    def _window(window, sinks):
+        """A window's width and first positions, in 32 bits."""
+        width = 0xFFFFFFFF if window is None else window
+        if not 1 <= width <= 0xFFFFFFFF or not 0 <= sinks <= 0xFFFFFFFF:
+            raise ValueError("window must be at least 1, or None; sinks must not be negative")
+        return width, sinks
+
+    def _row_floats(self, name, t, shape) -> int:
+        """The address of a contiguous float32 tensor [rows, heads]."""
+        if (t.dtype != self._float32 or t.device != self._device or t.shape != shape[:2]
+                or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 {list(shape[:2])} on {self._device}")
         return t.data_ptr()
 
     def _kv(self, layer, rows, ids, offsets):

@@ -10,8 +10,8 @@ import pytest
 from paper_2606_01387_amd import claimkv as ck
 from paper_2606_01387_amd import sequences
 
-STRUCTS = {"claim_rotate_desc": ck.CRotateDesc}
-PACKED = {ck.CRotateDesc: sequences._ROTATE}
+STRUCTS = {"claim_rotate_desc": ck.CRotateDesc, "claim_window_desc": ck.CWindowDesc}
+PACKED = {ck.CRotateDesc: sequences._ROTATE, ck.CWindowDesc: sequences._WINDOW}
 
 
 @pytest.fixture(scope="module")
@@ -62,5 +62,8 @@ def test_packed_records_are_the_structs(cls):
 
 
 def test_null_arguments_are_refused(L):
-    s = ctypes.addressof(ck.CSeqs())
+    s, need = ctypes.addressof(ck.CSeqs()), ctypes.c_uint64()
+    w = ctypes.addressof(ck.CWindowDesc())
+    assert L.claim_attend_window(None, s, w) == ck.EINVAL
+    assert L.claim_attend_window_work(None, s, w, ctypes.byref(need)) == ck.EINVAL
     assert L.claim_kv_write_rotated(None, s, ctypes.addressof(ck.CRotateDesc())) == ck.EINVAL
