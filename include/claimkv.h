@@ -718,6 +718,37 @@ int claim_attend_window_work(const claim_pool* pool, const claim_seqs* seqs, con
                              uint64_t* bytes);
 int claim_attend_window(claim_pool* pool, const claim_seqs* seqs, const claim_window_desc* desc);
 
+/* What each cached token weighed for the rows of a call: for every sequence r of
+ * the batch and position p below lengths[r] that has a block,
+ *   weights[r * weights_stride + p] += sum over r's rows that see p, and their
+ *     query heads, of exp(scale * k_scale * q . k_p - lse[row][head]),
+ * with the rows, window and sinks (window 2^32 - 1: all positions) of the call that
+ * gave lse; it may be given fewer of its rows (a prompt's last ones), with their
+ * lse.  A row and head whose lse is not finite adds nothing.  Weights, sums and lse
+ * are in 32 bits, and equal bits on every run, but for a sequence named twice, which
+ * gets both sums in either order.  Other entries of weights stay as they are.
+ *
+ * weights_stride is at least max_blocks * block_size; limits as for claim_attend, and
+ * max_blocks * block_size below 2^31.  work: claim_weigh_work bytes, 256-byte aligned
+ * (it goes by max_blocks and the counts alone; it may be 0, work NULL). */
+typedef struct claim_weigh_desc {
+  claim_kv_desc kv; /* v_scale is not used */
+  claim_rows q;
+  uint32_t num_heads;
+  uint32_t window; /* at least 1 */
+  uint32_t sinks;
+  float scale;
+  const float* lse; /* [num_rows][num_heads] */
+  float* weights;   /* [max_seqs] rows */
+  uint64_t weights_stride;
+  void* work;
+  uint64_t work_bytes;
+} claim_weigh_desc;
+
+int claim_weigh_work(const claim_pool* pool, const claim_seqs* seqs, const claim_weigh_desc* desc,
+                     uint64_t* bytes);
+int claim_weigh(claim_pool* pool, const claim_seqs* seqs, const claim_weigh_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,7 +16,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SOURCE = os.path.join(_HERE, "csrc", "claimkv.hip")
-SOURCES = (SOURCE, *(os.path.join(_HERE, "csrc", name + ".hip") for name in ("blocks", "attend", "window", "rotate")))
+SOURCES = (SOURCE, *(os.path.join(_HERE, "csrc", name + ".hip") for name in ("blocks", "attend", "window", "weigh", "rotate")))
 LIBRARY = os.path.join(_HERE, "libclaimkv.so")
 INCLUDE = os.path.join(ROOT, "include")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -58,7 +58,7 @@ EXPORTS = ("claim_pool_create", "claim_pool_destroy", "claim_offload", "claim_re
            "claim_digest_grid", "claim_strerror", "claim_seqs_grow", "claim_seqs_fork",
            "claim_seqs_free", "claim_seqs_compact", "claim_blocks_copy", "claim_kv_write",
            "claim_kv_write_rotated", "claim_attend", "claim_attend_work",
-           "claim_attend_window", "claim_attend_window_work")
+           "claim_attend_window", "claim_attend_window_work", "claim_weigh", "claim_weigh_work")
 
 
 class PoolDesc(ctypes.Structure):
@@ -139,6 +139,14 @@ class CWindowDesc(ctypes.Structure):
                 ("lse", ctypes.c_void_p)]
 
 
+class CWeighDesc(ctypes.Structure):
+    _fields_ = [("kv", CKvDesc), ("q", CRows), ("num_heads", ctypes.c_uint32),
+                ("window", ctypes.c_uint32), ("sinks", ctypes.c_uint32), ("scale", ctypes.c_float),
+                ("lse", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("weights_stride", ctypes.c_uint64), ("work", ctypes.c_void_p),
+                ("work_bytes", ctypes.c_uint64)]
+
+
 assert ctypes.sizeof(PoolDesc) == 96 and ctypes.sizeof(CBatch) == 72
 assert OUTCOME_DTYPE.itemsize == 64 and EVENT_DTYPE.itemsize == 40 and LOOKUP_DTYPE.itemsize == 40
 
@@ -200,6 +208,8 @@ def lib() -> ctypes.CDLL:
             "claim_attend_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
             "claim_attend_window": ([vp, vp, vp], i32),
             "claim_attend_window_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
+            "claim_weigh": ([vp, vp, vp], i32),
+            "claim_weigh_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)

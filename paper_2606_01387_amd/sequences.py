@@ -14,7 +14,7 @@ import ctypes
 import struct
 
 from . import claimkv
-from .claimkv import CAttendDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWindowDesc, ENOSPC, OK, _check, _torch, lib
+from .claimkv import CAttendDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWeighDesc, CWindowDesc, ENOSPC, OK, _check, _torch, lib
 
 SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED = 0, 1, 2
 NONE = -1  # a table entry that names no block (0xFFFFFFFF in 32 bits)
@@ -26,6 +26,8 @@ _ATTEND = struct.Struct("<4I2Q2f6Q2IQfI2Q")
 assert _WRITE.size == ctypes.sizeof(CKvDesc) + 2 * ctypes.sizeof(CRows)
 _ROTATE = struct.Struct("<4I2Q2f12Q2I4Q4I2QfI")
 _WINDOW = struct.Struct(_ATTEND.format + "2IQ")
+_WEIGH = struct.Struct("<4I2Q2f3Q3If5Q")
+assert _WEIGH.size == ctypes.sizeof(CWeighDesc)
 assert _WINDOW.size == ctypes.sizeof(CWindowDesc)
 assert _ATTEND.size == ctypes.sizeof(CAttendDesc)
 assert _ROTATE.size == ctypes.sizeof(CRotateDesc)
@@ -233,6 +235,22 @@ class Sequences:
         return self._attend(layer, q, prefix, self._ints("prefix", prefix), prefix.numel(), ids,
                             offsets, scale, k_scale, v_scale, out)
 
+    def weigh(self, layer: int, q, lse, weights, *, window: int | None = None, sinks: int = 0, ids=None,
+              offsets=None, scale: float | None = None, k_scale: float = 1.0) -> None:
+        """claim_weigh: adds to ``weights`` (float32 [max_seqs, columns], a
+        column for every position that a table has) what each cached token weighed
+        for the rows of ``q``, whose logarithms ``lse`` :meth:`attend_window` gave
+        with the same window, sinks and scales.  ``q`` and ``lse`` may be a
+        prompt's last rows alone."""
+        shape = q.shape
+        if len(shape) != 3:
+            raise ValueError("q must be [rows, heads, head_dim]")
+        given = (*self._kv(layer, shape[0], ids, offsets), k_scale, 1.0, *self._rows("q", q, shape[1]), shape[1],
+                 *self._window(window, sinks), self._dim**-0.5 if scale is None else scale,
+                 self._row_floats("lse", lse, shape), *self._weights(weights))
+        with self.pool.ordered(self, q, lse, weights, ids, offsets):
+            self._with_work(_WEIGH, given, (), self._lib.claim_weigh, self._lib.claim_weigh_work)
+
     def _attend(self, layer, q, prefix, prefix_at, blocks, ids, offsets, scale, k_scale, v_scale, out,
                 window=None):
         pool, shape, L = self.pool, q.shape, self._lib
@@ -296,6 +314,15 @@ class Sequences:
         if not 1 <= width <= 0xFFFFFFFF or not 0 <= sinks <= 0xFFFFFFFF:
             raise ValueError("window must be at least 1, or None; sinks must not be negative")
         return width, sinks
+
+    def _weights(self, t):
+        """The address and row stride of tokens' weights."""
+        seqs, blocks = self.tables.shape
+        room = blocks * self.pool.geometry.block_size
+        if (t.dtype != self._float32 or t.device != self._device or t.dim() != 2 or t.shape[0] != seqs
+                or t.shape[1] < room or t.stride(1) != 1 or (seqs > 1 and t.stride(0) < room)):
+            raise ValueError(f"weights must be float32 [{seqs}, at least {room}] on {self._device}, rows contiguous")
+        return t.data_ptr(), max(t.stride(0), room)
 
     def _row_floats(self, name, t, shape) -> int:
         """The address of a contiguous float32 tensor [rows, heads]."""

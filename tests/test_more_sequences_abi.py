@@ -10,8 +10,10 @@ import pytest
 from paper_2606_01387_amd import claimkv as ck
 from paper_2606_01387_amd import sequences
 
-STRUCTS = {"claim_rotate_desc": ck.CRotateDesc, "claim_window_desc": ck.CWindowDesc}
-PACKED = {ck.CRotateDesc: sequences._ROTATE, ck.CWindowDesc: sequences._WINDOW}
+STRUCTS = {"claim_rotate_desc": ck.CRotateDesc, "claim_window_desc": ck.CWindowDesc,
+           "claim_weigh_desc": ck.CWeighDesc}
+PACKED = {ck.CRotateDesc: sequences._ROTATE, ck.CWindowDesc: sequences._WINDOW,
+          ck.CWeighDesc: sequences._WEIGH}
 
 
 @pytest.fixture(scope="module")
@@ -67,3 +69,6 @@ def test_null_arguments_are_refused(L):
     assert L.claim_attend_window(None, s, w) == ck.EINVAL
     assert L.claim_attend_window_work(None, s, w, ctypes.byref(need)) == ck.EINVAL
     assert L.claim_kv_write_rotated(None, s, ctypes.addressof(ck.CRotateDesc())) == ck.EINVAL
+    d = ctypes.addressof(ck.CWeighDesc())
+    assert L.claim_weigh(None, s, d) == ck.EINVAL
+    assert L.claim_weigh_work(None, s, d, ctypes.byref(need)) == ck.EINVAL
