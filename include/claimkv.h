@@ -749,6 +749,52 @@ int claim_weigh_work(const claim_pool* pool, const claim_seqs* seqs, const claim
                      uint64_t* bytes);
 int claim_weigh(claim_pool* pool, const claim_seqs* seqs, const claim_weigh_desc* desc);
 
+/* Sequences cut to `tokens` tokens by what they weighed.  Entry i is row r = ids[i]
+ * (NULL: row i).  With L = lengths[r] <= tokens nothing changes.  Else it keeps its
+ * first `sinks` tokens, its last `recent`, and of the others the tokens - sinks -
+ * recent with the largest weights[r * weights_stride + position] (of equal ones the
+ * first; NaN is below all), in their order, at positions 0 .. tokens - 1, in all
+ * layers.  Their weights come with them, and weights of positions tokens .. L - 1
+ * become 0 (the next tokens', which are written there); blocks past the last are
+ * given up as claim_seqs_free gives them up.  Keys stay as they were turned: the
+ * positions of later tokens are for the program to count (claim_rotate_desc's).
+ *
+ * A block is rewritten where it is if no other row names it and the program holds
+ * no count of its own in refs; else a free block, lowest first, in order of i, then
+ * of position, takes its place, so that sequences forked from this one, claims'
+ * held blocks and prefix lists keep theirs.  This goes for blocks from the first
+ * whose tokens change, and a last one that is not full, as it will be written.  A
+ * rewritten block no longer holds the identity that it was registered with; blocks
+ * before it keep theirs, and their bytes.
+ *
+ * status (may be NULL): CLAIM_SEQ_NO_BLOCKS where the blocks that entries 0 .. i
+ * need in place of shared ones are more than are free at the call, and entry i needs
+ * any; CLAIM_SEQ_REFUSED for a row out of range or named by an earlier entry, a
+ * length past the table, or a position without a block.  Such a sequence and its
+ * weights are as before.  kept[i * tokens + j] is the position that position j's
+ * token had, CLAIM_NONE from the sequence's new length on, and for an entry that
+ * is refused or gets no blocks.
+ *
+ * tokens is at least 1 and sinks + recent at most tokens; a token's bytes in a
+ * plane are a multiple of 8; weights_stride and max_blocks as for claim_weigh. */
+typedef struct claim_evict_desc {
+  uint32_t n; /* at most max_seqs */
+  uint32_t tokens;
+  uint32_t sinks;
+  uint32_t recent;
+  const uint32_t* ids;
+  float* weights;
+  uint64_t weights_stride;
+  uint32_t* kept;   /* [n][tokens] */
+  uint32_t* status; /* [n] or NULL */
+  void* work;       /* claim_seqs_evict_work bytes, 256-byte aligned */
+  uint64_t work_bytes;
+} claim_evict_desc;
+
+int claim_seqs_evict_work(const claim_pool* pool, const claim_seqs* seqs, const claim_evict_desc* desc,
+                          uint64_t* bytes);
+int claim_seqs_evict(claim_pool* pool, const claim_seqs* seqs, const claim_evict_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,7 +16,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SOURCE = os.path.join(_HERE, "csrc", "claimkv.hip")
-SOURCES = (SOURCE, *(os.path.join(_HERE, "csrc", name + ".hip") for name in ("blocks", "attend", "window", "weigh", "rotate")))
+SOURCES = (SOURCE, *(os.path.join(_HERE, "csrc", name + ".hip") for name in ("blocks", "attend", "window", "weigh", "evict", "rotate")))
 LIBRARY = os.path.join(_HERE, "libclaimkv.so")
 INCLUDE = os.path.join(ROOT, "include")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -58,7 +58,8 @@ EXPORTS = ("claim_pool_create", "claim_pool_destroy", "claim_offload", "claim_re
            "claim_digest_grid", "claim_strerror", "claim_seqs_grow", "claim_seqs_fork",
            "claim_seqs_free", "claim_seqs_compact", "claim_blocks_copy", "claim_kv_write",
            "claim_kv_write_rotated", "claim_attend", "claim_attend_work",
-           "claim_attend_window", "claim_attend_window_work", "claim_weigh", "claim_weigh_work")
+           "claim_attend_window", "claim_attend_window_work", "claim_weigh", "claim_weigh_work",
+           "claim_seqs_evict", "claim_seqs_evict_work")
 
 
 class PoolDesc(ctypes.Structure):
@@ -147,6 +148,13 @@ class CWeighDesc(ctypes.Structure):
                 ("work_bytes", ctypes.c_uint64)]
 
 
+class CEvictDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_uint32), ("tokens", ctypes.c_uint32), ("sinks", ctypes.c_uint32),
+                ("recent", ctypes.c_uint32), ("ids", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("weights_stride", ctypes.c_uint64), ("kept", ctypes.c_void_p),
+                ("status", ctypes.c_void_p), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_uint64)]
+
+
 assert ctypes.sizeof(PoolDesc) == 96 and ctypes.sizeof(CBatch) == 72
 assert OUTCOME_DTYPE.itemsize == 64 and EVENT_DTYPE.itemsize == 40 and LOOKUP_DTYPE.itemsize == 40
 
@@ -210,6 +218,8 @@ def lib() -> ctypes.CDLL:
             "claim_attend_window_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
             "claim_weigh": ([vp, vp, vp], i32),
             "claim_weigh_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
+            "claim_seqs_evict": ([vp, vp, vp], i32),
+            "claim_seqs_evict_work": ([vp, vp, vp, ctypes.POINTER(u64)], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)

@@ -14,7 +14,7 @@ import ctypes
 import struct
 
 from . import claimkv
-from .claimkv import CAttendDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWeighDesc, CWindowDesc, ENOSPC, OK, _check, _torch, lib
+from .claimkv import CAttendDesc, CEvictDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWeighDesc, CWindowDesc, ENOSPC, OK, _check, _torch, lib
 
 SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED = 0, 1, 2
 NONE = -1  # a table entry that names no block (0xFFFFFFFF in 32 bits)
@@ -28,6 +28,8 @@ _ROTATE = struct.Struct("<4I2Q2f12Q2I4Q4I2QfI")
 _WINDOW = struct.Struct(_ATTEND.format + "2IQ")
 _WEIGH = struct.Struct("<4I2Q2f3Q3If5Q")
 assert _WEIGH.size == ctypes.sizeof(CWeighDesc)
+_EVICT = struct.Struct("<4I7Q")
+assert _EVICT.size == ctypes.sizeof(CEvictDesc)
 assert _WINDOW.size == ctypes.sizeof(CWindowDesc)
 assert _ATTEND.size == ctypes.sizeof(CAttendDesc)
 assert _ROTATE.size == ctypes.sizeof(CRotateDesc)
@@ -127,6 +129,23 @@ class Sequences:
             _check(self._lib.claim_seqs_compact(pool._h, self._seqs_ref, moved.data_ptr()),
                    "claim_seqs_compact")
         return moved
+
+    def evict(self, ids, weights, tokens: int, *, sinks: int = 0, recent: int = 0):
+        """claim_seqs_evict: sequences ``ids`` (None: all) that have more than
+        ``tokens`` tokens keep the first ``sinks``, the last ``recent`` and of the
+        others those of the largest ``weights`` (float32, as for :meth:`weigh`;
+        they come along).  Returns the device tensors of statuses and of the
+        kept tokens' old positions [n, tokens] (NONE past the new lengths)."""
+        at = 0 if ids is None else self._ints("ids", ids)
+        n = self.tables.shape[0] if ids is None else ids.numel()
+        if not 1 <= tokens < 1 << 31 or sinks < 0 or recent < 0 or sinks + recent > tokens:
+            raise ValueError("tokens must be at least 1, and sinks and recent not more than that together")
+        weights_at, stride = self._weights(weights)
+        status, kept = self.lengths.new_empty(n), self.lengths.new_empty(n, tokens)
+        given = (n, tokens, sinks, recent, at, weights_at, stride, kept.data_ptr(), status.data_ptr())
+        with self.pool.ordered(self, ids, weights, status, kept):
+            self._with_work(_EVICT, given, (), self._lib.claim_seqs_evict, self._lib.claim_seqs_evict_work)
+        return status, kept
 
     # ---------------------------------------------------- keys and values
     def write(self, layer: int, k, v, *, ids=None, offsets=None, k_scale: float = 1.0,

@@ -11,9 +11,9 @@ from paper_2606_01387_amd import claimkv as ck
 from paper_2606_01387_amd import sequences
 
 STRUCTS = {"claim_rotate_desc": ck.CRotateDesc, "claim_window_desc": ck.CWindowDesc,
-           "claim_weigh_desc": ck.CWeighDesc}
+           "claim_weigh_desc": ck.CWeighDesc, "claim_evict_desc": ck.CEvictDesc}
 PACKED = {ck.CRotateDesc: sequences._ROTATE, ck.CWindowDesc: sequences._WINDOW,
-          ck.CWeighDesc: sequences._WEIGH}
+          ck.CWeighDesc: sequences._WEIGH, ck.CEvictDesc: sequences._EVICT}
 
 
 @pytest.fixture(scope="module")
@@ -72,3 +72,6 @@ def test_null_arguments_are_refused(L):
     d = ctypes.addressof(ck.CWeighDesc())
     assert L.claim_weigh(None, s, d) == ck.EINVAL
     assert L.claim_weigh_work(None, s, d, ctypes.byref(need)) == ck.EINVAL
+    d = ctypes.addressof(ck.CEvictDesc())
+    assert L.claim_seqs_evict(None, s, d) == ck.EINVAL
+    assert L.claim_seqs_evict_work(None, s, d, ctypes.byref(need)) == ck.EINVAL
