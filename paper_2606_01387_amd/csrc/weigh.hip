@@ -212,13 +212,59 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 // ------------------------------------------------------------- many columns
 //
 // Eight waves of 64 keys each of one KV head take a chunk of the sequence's columns,
-// 64 at a time through LDS, two such tiles on their way.
+// 64 at a time through LDS, in two halves: while one half's scores become weights on
+// the vector unit, the matrix cores make those of the next.  A ring of three tiles:
+// two are on their way while one is read.
 
 constexpr uint32_t kManyKeys = 512, kManyColumns = 64;
 
 template <int D>
 struct WeighMany {
   static constexpr int kTile = kManyColumns * D * 2, kRing = 3;
+  static constexpr int kCopies = kTile / 8192 + 1;  // of a wave, for a tile
+};
+
+// 64 lanes copy 4 bytes each to LDS from `to` on (see copy_to_lds).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy_words_to_lds(const float* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               :
+               : "v"(from), "s"(to)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// A lane's column in one tile after another, and what belongs to it: no product is
+// left for the tiles' own loop.
+struct Walker {
+  uint32_t row, head;
+  uint64_t at, base;
+
+  template <typename T>
+  __device__ __forceinline__ void start(const WeighArgs& a, uint32_t x, const T* from, uint64_t row_stride,
+                                        uint64_t head_stride) {
+    row = quotient(x, a.group, a.group_magic);
+    head = x - row * a.group;
+    base = (uint64_t)from;
+    at = base + (row * row_stride + head * head_stride) * sizeof(T);
+  }
+
+  // This tile's place (past the rows: the first row's), and on to the next.
+  template <typename T>
+  __device__ __forceinline__ const uint8_t* next(const WeighArgs& a, const Item& it, uint32_t add_rows,
+                                                 uint32_t add_heads, uint64_t row_stride, uint64_t head_stride) {
+    const uint64_t got = row < it.n ? at : base;
+    row += add_rows;
+    head += add_heads;
+    at += (add_rows * row_stride + add_heads * head_stride) * sizeof(T);
+    if (head >= a.group) {
+      head -= a.group;
+      ++row;
+      at += (row_stride - a.group * head_stride) * sizeof(T);
+    }
+    return (const uint8_t*)got;
+  }
 };
 
 template <int D, bool E4M3>
@@ -226,6 +272,7 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
   using F = WeighMany<D>;
   constexpr int kBytes = D * (E4M3 ? 1 : 2), kSteps = D / 16;
   __shared__ __align__(1024) uint8_t ring[F::kRing * F::kTile];
+  __shared__ float sums[F::kRing][kManyColumns];  // the columns' logarithms
   const uint32_t t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6), half = lane >> 5;
   uint32_t b = blockIdx.x;
   const uint32_t h = b % a.heads;
@@ -249,11 +296,35 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
   const uint32_t x_first = from < to ? (uint32_t)from * a.group / kManyColumns : 0;
   const uint32_t x_end = from < to ? ((uint32_t)to * a.group + kManyColumns - 1) / kManyColumns : 0;
   const uint32_t share = (x_end - x_first + a.chunks - 1) / a.chunks;
-  uint32_t n = x_first + share * chunk < x_end ? x_first + share * chunk : x_end;
-  const uint32_t end = x_end - n < share ? x_end : n + share;
+  uint32_t n = uniform(x_first + share * chunk < x_end ? x_first + share * chunk : x_end);
+  const uint32_t end = uniform(x_end - n < share ? x_end : n + share);
   f32x16 acc[2] = {};
   if (n < end) {
     const uint32_t* table = a.tables + (uint64_t)(it.id < a.max_seqs ? it.id : 0) * a.max_blocks;
+    // a tile's columns to LDS: whole rows, 16-byte chunks exchanged as keys' are; past
+    // the rows, any (they add nothing)
+    constexpr uint32_t kRowLanes = D / 8, kRows = 512 / kRowLanes, kLooks = kManyColumns / kRows;
+    const uint32_t add_rows = kManyColumns / a.group, add_heads = kManyColumns - add_rows * a.group;
+    Walker columns[kLooks], logs;
+#pragma unroll
+    for (uint32_t i = 0; i < kLooks; ++i) {
+      const uint32_t r = i * kRows + t / kRowLanes;
+      columns[i].start(a, n * kManyColumns + r, (a.q + (uint64_t)it.first * a.q_row) + h * a.group * a.q_head +
+                       ((t % kRowLanes) ^ WideSwizzle<D>::k(r)) * 8, a.q_row, a.q_head);
+    }
+    const uint64_t all_heads = (uint64_t)a.heads * a.group;
+    logs.start(a, n * kManyColumns + lane, a.lse + it.first * all_heads + h * a.group, all_heads, 1);
+    const auto fetch = [&](uint32_t slot) {  // the next tile
+#pragma unroll
+      for (uint32_t i = 0; i < kLooks; ++i)
+        copy_to_lds(columns[i].template next<uint16_t>(a, it, add_rows, add_heads, a.q_row, a.q_head),
+                    lds_address(ring) + slot * F::kTile + i * 8192 + wave * 1024);
+      copy_words_to_lds((const float*)logs.template next<float>(a, it, add_rows, add_heads, all_heads, 1),
+                        lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
+    };
+    fetch(0);
+    fetch(1);
+    fetch(2);
     bf16x8 key[2][kSteps];
     bool there;
 #pragma unroll
@@ -271,65 +342,87 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
         key[u][i] = __builtin_bit_cast(bf16x8, w);
       }
     }
-    // a tile's columns to LDS: whole rows, 16-byte chunks exchanged as keys' are
-    constexpr uint32_t kRowLanes = D / 8, kRows = 512 / kRowLanes;
-    const auto fetch = [&](uint32_t m) {
+    const uint32_t lane_at = lds_address(ring) + (lane & 31) * D * 2 + ((half ^ WideSwizzle<D>::k(lane & 31)) << 4);
+    const auto multiply = [&](uint32_t slot, int c, f32x16 (&score)[2]) {
+      uint32_t at = slot * F::kTile + 32 * c * D * 2 + lane_at;
+      asm volatile("" : "+v"(at));
+      score[0] = score[1] = f32x16{};
 #pragma unroll
-      for (uint32_t i = 0; i < kManyColumns / kRows; ++i) {
-        const uint32_t r = i * kRows + t / kRowLanes, x = m * kManyColumns + r;
-        uint32_t row = quotient(x, a.group, a.group_magic);
-        const uint32_t head = h * a.group + (x - row * a.group);
-        row = row < it.n ? row : it.n - 1;  // past the rows: any, they add nothing
-        const uint16_t* src = a.q + (it.first + (uint64_t)row) * a.q_row + head * a.q_head +
-                              ((t % kRowLanes) ^ WideSwizzle<D>::k(r)) * 8;
-        copy_to_lds((const uint8_t*)src, lds_address(ring) + (m % F::kRing) * F::kTile + i * 8192 + wave * 1024);
+      for (int i = 0; i < kSteps; ++i) {
+        const u32x4 w = *(const lds_words*)(uintptr_t)(at ^ (i << 5));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w), score[u], 0, 0, 0);
       }
     };
-    fetch(n);
-    if (n + 1 < end) fetch(n + 1);
-    const uint32_t lane_at = (lane & 31) * D * 2 + ((half ^ WideSwizzle<D>::k(lane & 31)) << 4);
-    for (; n < end; ++n) {
-      Column col[2];
+    // the weights of half c of tile m
+    const auto weigh_some = [&](uint32_t m, int c, float lse, const f32x16 (&score)[2]) {
+      const float l = lse * kLog2e;
+      const uint32_t i = quotient(m * kManyColumns + 32 * c + (lane & 31), a.group, a.group_magic);
+      const int64_t limit = before + i + 1;
+      Column col;
+      col.limit = fabsf(lse) < __builtin_inff() && i < it.n && limit > 0
+                      ? (uint32_t)(limit < 0xFFFFFFFF ? limit : 0xFFFFFFFF) : 0;
+      col.low = col.limit > a.window ? col.limit - a.window : 0;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) col[c] = column_at(a, it, h, n * kManyColumns + 32 * c + (lane & 31));
-      wait_loads();
-      meet();
-      if (n + 2 < end) fetch(n + 2);
-      const uint32_t i0 = quotient(n * kManyColumns, a.group, a.group_magic);
-      uint32_t i1 = quotient(n * kManyColumns + kManyColumns - 1, a.group, a.group_magic);
-      i1 = i1 < it.n ? i1 : it.n - 1;
-      if (!some_see(a, it, i0, i1, pos, (int64_t)pos + 63)) continue;
-      const bool full = all_see(a, it, i0, i1, pos, (int64_t)pos + 63);
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        f32x16 score[2] = {};
-        const uint32_t at = lds_address(ring) + (n % F::kRing) * F::kTile + 32 * c * D * 2 + lane_at;
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t p = pos + 32 * u + 8 * (r / 4) + 4 * half + r % 4;
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(score[u][r], a.c, -l));
+          acc[u][r] += sees(col, p, a.sinks) ? w : 0.0f;
+        }
+    };
+    // scores of half c at `slot`, while the half before them becomes weights
+    const auto both = [&](uint32_t slot, int c, f32x16 (&score)[2], uint32_t m, float lse, bool full,
+                          const f32x16 (&last)[2]) {
+      if (full && __all(fabsf(lse) < __builtin_inff())) {
+        // two products, then what the vector unit does meanwhile; operands are read two
+        // steps ahead
+        const float l = lse * kLog2e;
+        uint32_t at = slot * F::kTile + 32 * c * D * 2 + lane_at;
+        asm volatile("" : "+v"(at));
+        score[0] = score[1] = f32x16{};
+        u32x4 w[kSteps];
+        const auto read = [&](int i) { w[i] = *(const lds_words*)(uintptr_t)(at ^ (i << 5)); };
+        read(0);
+        read(1);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-          const u32x4 w = *(const lds_words*)(uintptr_t)(at ^ (i << 5));
+          if (i + 2 < kSteps) read(i + 2);
 #pragma unroll
           for (int u = 0; u < 2; ++u)
-            score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w), score[u], 0, 0, 0);
+            score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w[i]), score[u], 0, 0, 0);
+#pragma unroll
+          for (int e = 32 / kSteps * i; e < 32 / kSteps * (i + 1); ++e)
+            acc[e / 16][e % 16] += __builtin_amdgcn_exp2f(__builtin_fmaf(last[e / 16][e % 16], a.c, -l));
+          __builtin_amdgcn_sched_barrier(0);
         }
-        const bool counts = col[c].lse < __builtin_inff();
-        if (full && __all(counts)) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              acc[u][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(score[u][r], a.c, -col[c].lse));
-        } else {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const uint32_t p = pos + 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(score[u][r], a.c, -col[c].lse));
-              acc[u][r] += counts && sees(col[c], p, a.sinks) ? w : 0.0f;
-            }
-        }
+      } else {
+        multiply(slot, c, score);
+        weigh_some(m, 1 - c, lse, last);
       }
+    };
+    uint32_t slot = 0;
+    f32x16 one[2], two[2];
+    wait_copies<2 * F::kCopies>();
+    meet();
+    multiply(0, 0, one);
+    for (; n < end; ++n) {
+      const uint32_t i0 = quotient(n * kManyColumns, a.group, a.group_magic);
+      const uint32_t i1 = quotient(n * kManyColumns + kManyColumns - 1, a.group, a.group_magic);
+      const bool full = uniform(i1 < it.n && all_see(a, it, i0, i1, pos, (int64_t)pos + 63));
+      const float l0 = sums[slot][lane & 31], l1 = sums[slot][32 + (lane & 31)];
+      both(slot, 1, two, n, l0, full, one);
+      // tile n has been read, n + 1 is there
+      const uint32_t was = slot;
+      slot = slot == F::kRing - 1 ? 0 : slot + 1;
+      wait_copies<F::kCopies>();
+      meet();
+      fetch(was);
+      both(slot, 0, one, n, l1, full, two);  // (past the last: of columns that nobody weighs)
     }
+    wait_loads();  // no copy outlives the workgroup
   }
 #pragma unroll
   for (int u = 0; u < 2; ++u)
