@@ -211,17 +211,17 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 
 // ------------------------------------------------------------- many columns
 //
-// Eight waves of 64 keys each of one KV head take a chunk of the sequence's columns,
+// Four waves of 64 keys each of one KV head take a chunk of the sequence's columns,
 // 64 at a time through LDS, in two halves: while one half's scores become weights on
 // the vector unit, the matrix cores make those of the next.  A ring of three tiles:
 // two are on their way while one is read.
 
-constexpr uint32_t kManyKeys = 512, kManyColumns = 64;
+constexpr uint32_t kManyWaves = 4, kManyKeys = 64 * kManyWaves, kManyColumns = 64;
 
 template <int D>
 struct WeighMany {
   static constexpr int kTile = kManyColumns * D * 2, kRing = 3;
-  static constexpr int kCopies = kTile / 8192 + 1;  // of a wave, for a tile
+  static constexpr int kCopies = kTile / (1024 * kManyWaves) + 1;  // of a wave, for a tile
 };
 
 // 64 lanes copy 4 bytes each to LDS from `to` on (see copy_to_lds).
@@ -268,7 +268,7 @@ struct Walker {
 };
 
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
+__global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) {
   using F = WeighMany<D>;
   constexpr int kBytes = D * (E4M3 ? 1 : 2), kSteps = D / 16;
   __shared__ __align__(1024) uint8_t ring[F::kRing * F::kTile];
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
     const uint32_t* table = a.tables + (uint64_t)(it.id < a.max_seqs ? it.id : 0) * a.max_blocks;
     // a tile's columns to LDS: whole rows, 16-byte chunks exchanged as keys' are; past
     // the rows, any (they add nothing)
-    constexpr uint32_t kRowLanes = D / 8, kRows = 512 / kRowLanes, kLooks = kManyColumns / kRows;
+    constexpr uint32_t kRowLanes = D / 8, kRows = 64 * kManyWaves / kRowLanes, kLooks = kManyColumns / kRows;
     const uint32_t add_rows = kManyColumns / a.group, add_heads = kManyColumns - add_rows * a.group;
     Walker columns[kLooks], logs;
 #pragma unroll
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
 #pragma unroll
       for (uint32_t i = 0; i < kLooks; ++i)
         copy_to_lds(columns[i].template next<uint16_t>(a, it, add_rows, add_heads, a.q_row, a.q_head),
-                    lds_address(ring) + slot * F::kTile + i * 8192 + wave * 1024);
+                    lds_address(ring) + slot * F::kTile + (i * kManyWaves + wave) * 1024);
       copy_words_to_lds((const float*)logs.template next<float>(a, it, add_rows, add_heads, all_heads, 1),
                         lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
     };
@@ -403,24 +403,34 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
         weigh_some(m, 1 - c, lse, last);
       }
     };
+    // this wave's tiles: some row sees some key in seen_from .. seen_to - 1, every row
+    // every key in full_from .. full_to - 1
+    const auto at_least = [](int64_t x) { return x > 0 ? (uint64_t)x : 0; };
+    const uint64_t g = a.group, all = (uint64_t)it.n * g / kManyColumns;
+    const uint64_t seen_from = at_least(pos - before) * g / kManyColumns;
+    const uint64_t full_from = (at_least(pos + 63ll - before) * g + kManyColumns - 1) / kManyColumns;
+    uint64_t seen_to = ~0ull, full_to = ~0ull;
+    if (pos >= a.sinks) seen_to = (at_least(pos + 63ll - before + a.window) * g + kManyColumns - 1) / kManyColumns;
+    if (pos + 63 >= a.sinks) full_to = at_least((int64_t)pos - before + a.window) * g / kManyColumns;
+    full_to = full_to < all ? full_to : all;
+    const auto seen = [&](uint32_t m) { return m >= seen_from && m < seen_to; };
     uint32_t slot = 0;
     f32x16 one[2], two[2];
     wait_copies<2 * F::kCopies>();
     meet();
     multiply(0, 0, one);
     for (; n < end; ++n) {
-      const uint32_t i0 = quotient(n * kManyColumns, a.group, a.group_magic);
-      const uint32_t i1 = quotient(n * kManyColumns + kManyColumns - 1, a.group, a.group_magic);
-      const bool full = uniform(i1 < it.n && all_see(a, it, i0, i1, pos, (int64_t)pos + 63));
+      const bool full = n >= full_from && n < full_to;
       const float l0 = sums[slot][lane & 31], l1 = sums[slot][32 + (lane & 31)];
-      both(slot, 1, two, n, l0, full, one);
+      if (seen(n)) both(slot, 1, two, n, l0, full, one);
       // tile n has been read, n + 1 is there
       const uint32_t was = slot;
       slot = slot == F::kRing - 1 ? 0 : slot + 1;
       wait_copies<F::kCopies>();
       meet();
       fetch(was);
-      both(slot, 0, one, n, l1, full, two);  // (past the last: of columns that nobody weighs)
+      // (past the last: of columns that nobody weighs)
+      if (seen(n) || seen(n + 1)) both(slot, 0, one, n, l1, full, two);
     }
     wait_loads();  // no copy outlives the workgroup
   }
@@ -440,18 +450,25 @@ __global__ void __launch_bounds__(512, 2) k_weigh_rows(WeighArgs a) {
       }
 }
 
-// Parts of a position, head by head, chunk by chunk.
-__global__ void __launch_bounds__(256) k_weigh_join(WeighArgs a, uint32_t groups) {
+// Parts of a position, in order: eight loads on their way at a time.
+__global__ void __launch_bounds__(64) k_weigh_join(WeighArgs a, uint32_t groups) {
   const uint32_t s = blockIdx.x / groups;
   const Item it = item_at(a, s);
   const uint32_t* table = a.tables + (uint64_t)(it.id < a.max_seqs ? it.id : 0) * a.max_blocks;
   const uint32_t parts = a.heads * a.chunks;
-  for (uint64_t p = (uint64_t)(blockIdx.x - s * groups) * 256 + threadIdx.x; p < it.keys; p += (uint64_t)groups * 256) {
+  const uint64_t stride = (uint64_t)a.num_seqs * a.room;
+  for (uint64_t p = (uint64_t)(blockIdx.x - s * groups) * 64 + threadIdx.x; p < it.keys; p += (uint64_t)groups * 64) {
     const float* part = a.parts + (uint64_t)s * a.room + p;
-    float sum = 0;
-    for (uint32_t i = 0; i < parts; ++i) sum += part[(uint64_t)i * a.num_seqs * a.room];
     bool there;
     key_row(a, table, (uint32_t)p, &there);
+    float sum = 0;
+    for (uint32_t i = 0; i < parts; i += 8) {
+      float x[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) x[j] = i + j < parts ? part[(i + j) * stride] : 0.0f;
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) sum += x[j];
+    }
     if (there && sum != 0.0f) unsafeAtomicAdd(a.weights + it.id * a.weights_row + p, sum);
   }
 }
@@ -500,7 +517,7 @@ int check_weigh(const PoolView& p, const claim_seqs* s, const claim_weigh_desc* 
   if (d->kv.num_rows == 0) return CLAIM_OK;
   const WeighPlan plan = make_weigh_plan(p, s, d);
   const uint64_t groups = (uint64_t)plan.tiles * plan.chunks * d->kv.num_seqs * p.heads;
-  return plan.many && groups >= 1u << 23 ? CLAIM_EINVAL : CLAIM_OK;  // 2^32 threads
+  return plan.many && groups >= 1u << 24 ? CLAIM_EINVAL : CLAIM_OK;  // 2^32 threads
 }
 
 template <int D, bool E4M3>
@@ -508,11 +525,11 @@ int launch(const PoolView& p, const WeighPlan& plan, const WeighArgs& a) {
   if (!plan.many) {
     hipLaunchKernelGGL((k_weigh_few<D, E4M3>), dim3(a.num_seqs * a.tiles), dim3(256), 0, p.stream, a);
   } else {
-    hipLaunchKernelGGL((k_weigh_rows<D, E4M3>), dim3(a.num_seqs * a.tiles * a.chunks * a.heads), dim3(512), 0,
+    hipLaunchKernelGGL((k_weigh_rows<D, E4M3>), dim3(a.num_seqs * a.tiles * a.chunks * a.heads), dim3(64 * kManyWaves), 0,
                        p.stream, a);
-    const uint32_t most = 8 * p.cus / a.num_seqs + 1, need = (a.room + 255) / 256;
+    const uint32_t most = 32 * p.cus / a.num_seqs + 1, need = (a.room + 63) / 64;
     const uint32_t groups = need < most ? need : most;
-    hipLaunchKernelGGL(k_weigh_join, dim3(a.num_seqs * groups), dim3(256), 0, p.stream, a, groups);
+    hipLaunchKernelGGL(k_weigh_join, dim3(a.num_seqs * groups), dim3(64), 0, p.stream, a, groups);
   }
   return hipGetLastError() == hipSuccess ? CLAIM_OK : CLAIM_EHIP;
 }
