@@ -214,7 +214,9 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 // Four waves of 64 keys each of one KV head take a chunk of the sequence's columns,
 // 64 at a time through LDS, in two halves: while one half's scores become weights on
 // the vector unit, the matrix cores make those of the next.  A ring of three tiles:
-// two are on their way while one is read.
+// two are on their way while one is read.  A tile is as many whole rows as 64 columns
+// hold (63 columns of a group of 7), so that a lane's place in it is the same in
+// every tile.
 
 constexpr uint32_t kManyWaves = 4, kManyKeys = 64 * kManyWaves, kManyColumns = 64;
 
@@ -227,45 +229,13 @@ struct WeighMany {
 // 64 lanes copy 4 bytes each to LDS from `to` on (see copy_to_lds).
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void copy_words_to_lds(const float* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+__device__ __forceinline__ void copy_words_to_lds(const uint8_t* base, uint32_t lane_offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
                :
-               : "v"(from), "s"(to)
+               : "v"(lane_offset), "s"(base), "s"(to)
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
-
-// A lane's column in one tile after another, and what belongs to it: no product is
-// left for the tiles' own loop.
-struct Walker {
-  uint32_t row, head;
-  uint64_t at, base;
-
-  template <typename T>
-  __device__ __forceinline__ void start(const WeighArgs& a, uint32_t x, const T* from, uint64_t row_stride,
-                                        uint64_t head_stride) {
-    row = quotient(x, a.group, a.group_magic);
-    head = x - row * a.group;
-    base = (uint64_t)from;
-    at = base + (row * row_stride + head * head_stride) * sizeof(T);
-  }
-
-  // This tile's place (past the rows: the first row's), and on to the next.
-  template <typename T>
-  __device__ __forceinline__ const uint8_t* next(const WeighArgs& a, const Item& it, uint32_t add_rows,
-                                                 uint32_t add_heads, uint64_t row_stride, uint64_t head_stride) {
-    const uint64_t got = row < it.n ? at : base;
-    row += add_rows;
-    head += add_heads;
-    at += (add_rows * row_stride + add_heads * head_stride) * sizeof(T);
-    if (head >= a.group) {
-      head -= a.group;
-      ++row;
-      at += (row_stride - a.group * head_stride) * sizeof(T);
-    }
-    return (const uint8_t*)got;
-  }
-};
 
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) {
@@ -285,46 +255,55 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
   float* part = a.parts + (((uint64_t)h * a.chunks + chunk) * a.num_seqs + s) * a.room;
   const uint32_t base = tile * kManyKeys, pos = base + wave * 64;  // this wave's keys
   const int64_t before = it.len - it.n;
-  // the rows that see any of the workgroup's keys
+  // the tiles of rows that see any of the workgroup's keys, and this chunk's of them
+  const uint32_t rows = kManyColumns / a.group;  // of a tile
   int64_t from = (int64_t)base - before, to = it.n;
   if (base >= a.sinks) {
     const int64_t last = (int64_t)base + kManyKeys - 1 - before + a.window;  // the first row past all of them
     to = last < to ? last : to;
   }
   from = from > 0 ? from : 0;
-  // this chunk's columns of them, in whole tiles
-  const uint32_t x_first = from < to ? (uint32_t)from * a.group / kManyColumns : 0;
-  const uint32_t x_end = from < to ? ((uint32_t)to * a.group + kManyColumns - 1) / kManyColumns : 0;
-  const uint32_t share = (x_end - x_first + a.chunks - 1) / a.chunks;
-  uint32_t n = uniform(x_first + share * chunk < x_end ? x_first + share * chunk : x_end);
-  const uint32_t end = uniform(x_end - n < share ? x_end : n + share);
+  const uint32_t first = from < to ? (uint32_t)from / rows : 0;
+  const uint32_t past = from < to ? ((uint32_t)to + rows - 1) / rows : 0;
+  const uint32_t share = (past - first + a.chunks - 1) / a.chunks;
+  uint32_t n = uniform(first + share * chunk < past ? first + share * chunk : past);
+  const uint32_t end = uniform(past - n < share ? past : n + share);
   f32x16 acc[2] = {};
   if (n < end) {
     const uint32_t* table = a.tables + (uint64_t)(it.id < a.max_seqs ? it.id : 0) * a.max_blocks;
-    // a tile's columns to LDS: whole rows, 16-byte chunks exchanged as keys' are; past
-    // the rows, any (they add nothing)
+    // a tile's columns to LDS: whole rows, 16-byte chunks exchanged as keys' are.  Columns
+    // past the tile's rows, or in the last tile past the sequence's, read the first
+    // one's, and add nothing.
     constexpr uint32_t kRowLanes = D / 8, kRows = 64 * kManyWaves / kRowLanes, kLooks = kManyColumns / kRows;
-    const uint32_t add_rows = kManyColumns / a.group, add_heads = kManyColumns - add_rows * a.group;
-    Walker columns[kLooks], logs;
+    const uint64_t all_heads = (uint64_t)a.heads * a.group;
+    const uint32_t last = (it.n - 1) / rows, left = it.n - last * rows;  // of the last tile
+    uint32_t look[kLooks], look_last[kLooks], log, log_last;
 #pragma unroll
     for (uint32_t i = 0; i < kLooks; ++i) {
-      const uint32_t r = i * kRows + t / kRowLanes;
-      columns[i].start(a, n * kManyColumns + r, (a.q + (uint64_t)it.first * a.q_row) + h * a.group * a.q_head +
-                       ((t % kRowLanes) ^ WideSwizzle<D>::k(r)) * 8, a.q_row, a.q_head);
+      const uint32_t r = i * kRows + t / kRowLanes, row = quotient(r, a.group, a.group_magic);
+      const uint32_t at = (row * (uint32_t)a.q_row + (r - row * a.group) * (uint32_t)a.q_head) * 2;
+      const uint32_t in = ((t % kRowLanes) ^ WideSwizzle<D>::k(r)) * 16;
+      look[i] = in + (row < rows ? at : 0);
+      look_last[i] = in + (row < left ? at : 0);
     }
-    const uint64_t all_heads = (uint64_t)a.heads * a.group;
-    logs.start(a, n * kManyColumns + lane, a.lse + it.first * all_heads + h * a.group, all_heads, 1);
-    const auto fetch = [&](uint32_t slot) {  // the next tile
+    const uint32_t lane_row = quotient(lane, a.group, a.group_magic);
+    log = lane_row < rows ? (lane_row * (uint32_t)all_heads + lane - lane_row * a.group) * 4 : 0;
+    log_last = lane_row < left ? log : 0;
+    const uint8_t* q = (const uint8_t*)(a.q + it.first * a.q_row + h * a.group * a.q_head);
+    const uint8_t* lse = (const uint8_t*)(a.lse + it.first * all_heads + h * a.group);
+    const auto fetch = [&](uint32_t m, uint32_t slot) {
+      const bool ends = m >= last;
+      const uint64_t row = (uint64_t)(ends ? last : m) * rows;
+      const uint8_t *from = uniform(q + row * a.q_row * 2), *sums_from = uniform(lse + row * all_heads * 4);
 #pragma unroll
       for (uint32_t i = 0; i < kLooks; ++i)
-        copy_to_lds(columns[i].template next<uint16_t>(a, it, add_rows, add_heads, a.q_row, a.q_head),
+        copy_to_lds(from, ends ? look_last[i] : look[i],
                     lds_address(ring) + slot * F::kTile + (i * kManyWaves + wave) * 1024);
-      copy_words_to_lds((const float*)logs.template next<float>(a, it, add_rows, add_heads, all_heads, 1),
-                        lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
+      copy_words_to_lds(sums_from, ends ? log_last : log, lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
     };
-    fetch(0);
-    fetch(1);
-    fetch(2);
+    fetch(n, 0);
+    fetch(n + 1, 1);
+    fetch(n + 2, 2);
     bf16x8 key[2][kSteps];
     bool there;
 #pragma unroll
@@ -356,12 +335,13 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       }
     };
     // the weights of half c of tile m
+    const uint32_t half_row[2] = {quotient(lane & 31, a.group, a.group_magic),
+                                  quotient(32 + (lane & 31), a.group, a.group_magic)};
     const auto weigh_some = [&](uint32_t m, int c, float lse, const f32x16 (&score)[2]) {
       const float l = lse * kLog2e;
-      const uint32_t i = quotient(m * kManyColumns + 32 * c + (lane & 31), a.group, a.group_magic);
-      const int64_t limit = before + i + 1;
+      const int64_t i = (int64_t)m * rows + half_row[c], limit = before + i + 1;
       Column col;
-      col.limit = fabsf(lse) < __builtin_inff() && i < it.n && limit > 0
+      col.limit = fabsf(lse) < __builtin_inff() && half_row[c] < rows && i < it.n && limit > 0
                       ? (uint32_t)(limit < 0xFFFFFFFF ? limit : 0xFFFFFFFF) : 0;
       col.low = col.limit > a.window ? col.limit - a.window : 0;
 #pragma unroll
@@ -379,7 +359,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       if (full && __all(fabsf(lse) < __builtin_inff())) {
         // two products, then what the vector unit does meanwhile; operands are read two
         // steps ahead
-        const float l = lse * kLog2e;
+        const float l = half_row[1 - c] < rows ? lse * kLog2e : __builtin_inff();
         uint32_t at = slot * F::kTile + 32 * c * D * 2 + lane_at;
         asm volatile("" : "+v"(at));
         score[0] = score[1] = f32x16{};
@@ -405,14 +385,18 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
     };
     // this wave's tiles: some row sees some key in seen_from .. seen_to - 1, every row
     // every key in full_from .. full_to - 1
-    const auto at_least = [](int64_t x) { return x > 0 ? (uint64_t)x : 0; };
-    const uint64_t g = a.group, all = (uint64_t)it.n * g / kManyColumns;
-    const uint64_t seen_from = at_least(pos - before) * g / kManyColumns;
-    const uint64_t full_from = (at_least(pos + 63ll - before) * g + kManyColumns - 1) / kManyColumns;
-    uint64_t seen_to = ~0ull, full_to = ~0ull;
-    if (pos >= a.sinks) seen_to = (at_least(pos + 63ll - before + a.window) * g + kManyColumns - 1) / kManyColumns;
-    if (pos + 63 >= a.sinks) full_to = at_least((int64_t)pos - before + a.window) * g / kManyColumns;
-    full_to = full_to < all ? full_to : all;
+    const auto down = [&](int64_t x) { return x > 0 ? (x < 0xFFFFFFFF ? (uint32_t)x : 0xFFFFFFFFu) / rows : 0; };
+    const auto up = [&](int64_t x) { return down(x + rows - 1); };
+    uint32_t seen_from = down(pos - before), full_from = up(pos + 63ll - before), seen_to = ~0u, full_to = it.n / rows;
+    if (pos >= a.sinks) seen_to = up(pos + 63ll - before + a.window);
+    if (pos + 63 >= a.sinks) {
+      const uint32_t x = down((int64_t)pos - before + a.window);
+      full_to = x < full_to ? x : full_to;
+    }
+    seen_from = uniform(seen_from);
+    full_from = uniform(full_from);
+    seen_to = uniform(seen_to);
+    full_to = uniform(full_to);
     const auto seen = [&](uint32_t m) { return m >= seen_from && m < seen_to; };
     uint32_t slot = 0;
     f32x16 one[2], two[2];
@@ -428,7 +412,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       slot = slot == F::kRing - 1 ? 0 : slot + 1;
       wait_copies<F::kCopies>();
       meet();
-      fetch(was);
+      fetch(n + 3, was);
       // (past the last: of columns that nobody weighs)
       if (seen(n) || seen(n + 1)) both(slot, 0, one, n, l1, full, two);
     }
@@ -484,7 +468,9 @@ WeighPlan make_weigh_plan(const PoolView& p, const claim_seqs* s, const claim_we
   WeighPlan r{};
   const uint64_t group = d->num_heads / p.heads, rows = d->kv.num_rows, seqs = d->kv.num_seqs;
   const uint64_t room = (uint64_t)s->max_blocks * p.bs;
-  r.many = (rows * group + seqs - 1) / seqs > 64;
+  // k_weigh_rows keeps places within 64 rows in 32 bits
+  const bool near = d->q.row_stride < 1u << 24 && d->q.head_stride < 1u << 24;
+  r.many = (rows * group + seqs - 1) / seqs > 64 && near;
   r.chunks = 1;
   if (!r.many) {
     const uint64_t span = p.heads >= 4 ? 64 : p.heads >= 2 ? 128 : 256;
