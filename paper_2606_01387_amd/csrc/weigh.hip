@@ -112,6 +112,19 @@ __device__ __forceinline__ const uint8_t* key_row(const WeighArgs& a, const uint
   return a.k + (uint64_t)(*there ? entry : 0) * a.chunk_bytes + (uint64_t)(*there ? token : 0) * a.token_bytes;
 }
 
+// A value's sum over 16 neighbouring lanes, on all of them: pairs, fours, then halves
+// mirrored, within the vector unit (by shuffles through LDS, a workgroup of
+// k_weigh_rows took 6 us for its beginning and end).
+__device__ __forceinline__ float sum16(float x) {
+  const auto add = [](float v, auto how) {
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), decltype(how)::value, 15, 15, true));
+  };
+  x = add(x, std::integral_constant<int, 0xB1>{});   // lane ^ 1
+  x = add(x, std::integral_constant<int, 0x4E>{});   // lane ^ 2
+  x = add(x, std::integral_constant<int, 0x141>{});  // 7 - lane of eight
+  return add(x, std::integral_constant<int, 0x140>{});  // 15 - lane of sixteen
+}
+
 // -------------------------------------------------------------- few columns
 //
 // Four waves share the KV heads of 64 keys (of 128 or 256, where there are two heads
@@ -189,12 +202,11 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) acc[n][r] += __shfl_xor(acc[n][r], d);
+      for (int r = 0; r < 4; ++r) acc[n][r] = sum16(acc[n][r]);
     if (x == 0)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) *(f32x4*)(sums + wave * 64 + 16 * n + 4 * g) = f32x4{acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
+      for (int n = 0; n < 4; ++n)
+        *(f32x4*)(sums + wave * 64 + 16 * n + 4 * g) = f32x4{acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
     __syncthreads();
     const uint32_t t = threadIdx.x;
     if (t < span && tile * span + t < it.keys) {
@@ -421,9 +433,11 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) acc[u][r] += __shfl_xor(acc[u][r], d);
+    for (int r = 0; r < 16; ++r) {
+      float x = sum16(acc[u][r]);
+      const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      acc[u][r] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
   if ((lane & 31) == 0)
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -480,7 +494,7 @@ WeighPlan make_weigh_plan(const PoolView& p, const claim_seqs* s, const claim_we
   }
   r.tiles = (uint32_t)((room + kManyKeys - 1) / kManyKeys);
   const uint64_t groups = (uint64_t)r.tiles * seqs * p.heads, columns = rows * group / seqs;
-  while (r.chunks < 32 && groups * r.chunks < 4ull * p.cus && columns / r.chunks > 512) r.chunks *= 2;
+  while (r.chunks < 32 && groups * r.chunks < 8ull * p.cus && columns / r.chunks > 512) r.chunks *= 2;
   return r;
 }
 
