@@ -225,8 +225,8 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 //
 // Four waves of 64 keys each of one KV head take a chunk of the sequence's columns,
 // 64 at a time through LDS, in two halves: while one half's scores become weights on
-// the vector unit, the matrix cores make those of the next.  A ring of three tiles:
-// two are on their way while one is read.  A tile is as many whole rows as 64 columns
+// the vector unit, the matrix cores make those of the next.  A ring of four tiles:
+// two are on their way while one is read and one is there.  A tile is as many whole rows as 64 columns
 // hold (63 columns of a group of 7), so that a lane's place in it is the same in
 // every tile.
 
@@ -234,7 +234,7 @@ constexpr uint32_t kManyWaves = 4, kManyKeys = 64 * kManyWaves, kManyColumns = 6
 
 template <int D>
 struct WeighMany {
-  static constexpr int kTile = kManyColumns * D * 2, kRing = 3;
+  static constexpr int kTile = kManyColumns * D * 2, kRing = 4;
   static constexpr int kCopies = kTile / (1024 * kManyWaves) + 1;  // of a wave, for a tile
 };
 
@@ -289,18 +289,20 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
     constexpr uint32_t kRowLanes = D / 8, kRows = 64 * kManyWaves / kRowLanes, kLooks = kManyColumns / kRows;
     const uint64_t all_heads = (uint64_t)a.heads * a.group;
     const uint32_t last = (it.n - 1) / rows, left = it.n - last * rows;  // of the last tile
-    uint32_t look[kLooks], look_last[kLooks], log, log_last;
+    uint32_t look[kLooks], log;
+    bool has[kLooks], has_log;  // in the last tile
+    const uint32_t chunk_at = ((t % kRowLanes) ^ WideSwizzle<D>::k(t / kRowLanes)) * 16;  // kRows on: the same
 #pragma unroll
     for (uint32_t i = 0; i < kLooks; ++i) {
       const uint32_t r = i * kRows + t / kRowLanes, row = quotient(r, a.group, a.group_magic);
       const uint32_t at = (row * (uint32_t)a.q_row + (r - row * a.group) * (uint32_t)a.q_head) * 2;
-      const uint32_t in = ((t % kRowLanes) ^ WideSwizzle<D>::k(r)) * 16;
-      look[i] = in + (row < rows ? at : 0);
-      look_last[i] = in + (row < left ? at : 0);
+      static_assert(WideSwizzle<D>::k(kRows) == 0, "");
+      look[i] = chunk_at + (row < rows ? at : 0);
+      has[i] = row < left;
     }
     const uint32_t lane_row = quotient(lane, a.group, a.group_magic);
     log = lane_row < rows ? (lane_row * (uint32_t)all_heads + lane - lane_row * a.group) * 4 : 0;
-    log_last = lane_row < left ? log : 0;
+    has_log = lane_row < left;
     const uint8_t* q = (const uint8_t*)(a.q + it.first * a.q_row + h * a.group * a.q_head);
     const uint8_t* lse = (const uint8_t*)(a.lse + it.first * all_heads + h * a.group);
     const auto fetch = [&](uint32_t m, uint32_t slot) {
@@ -309,9 +311,9 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       const uint8_t *from = uniform(q + row * a.q_row * 2), *sums_from = uniform(lse + row * all_heads * 4);
 #pragma unroll
       for (uint32_t i = 0; i < kLooks; ++i)
-        copy_to_lds(from, ends ? look_last[i] : look[i],
+        copy_to_lds(from, ends && !has[i] ? chunk_at : look[i],
                     lds_address(ring) + slot * F::kTile + (i * kManyWaves + wave) * 1024);
-      copy_words_to_lds(sums_from, ends ? log_last : log, lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
+      copy_words_to_lds(sums_from, ends && !has_log ? 0 : log, lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
     };
     fetch(n, 0);
     fetch(n + 1, 1);
@@ -334,66 +336,56 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       }
     }
     const uint32_t lane_at = lds_address(ring) + (lane & 31) * D * 2 + ((half ^ WideSwizzle<D>::k(lane & 31)) << 4);
-    const auto multiply = [&](uint32_t slot, int c, f32x16 (&score)[2]) {
-      uint32_t at = slot * F::kTile + 32 * c * D * 2 + lane_at;
-      asm volatile("" : "+v"(at));
+    // a half's operands; the first two are read before the half before it is done
+    u32x4 w[kSteps];
+    const auto read = [&](uint32_t at, int i) { w[i] = *(const lds_words*)(uintptr_t)(at ^ (i << 5)); };
+    const auto place = [&](uint32_t slot, int c) { return slot * F::kTile + 32 * c * D * 2 + lane_at; };
+    // The scores of a half at `at`, while the last half's (half c of tile m, with the
+    // columns' logarithms `lse`) become weights: of keys that all see, of keys up to the
+    // columns' own, or of any.  Two products, then what the vector unit does
+    // meanwhile; operands are read two steps ahead, `after`'s in the end.
+    const uint32_t half_row[2] = {quotient(lane & 31, a.group, a.group_magic),
+                                  quotient(32 + (lane & 31), a.group, a.group_magic)};
+    const bool causal = a.window == ~0u;
+    const auto step = [&](auto mode, uint32_t at, uint32_t after, f32x16 (&score)[2], float l, uint32_t limit,
+                          const f32x16 (&last)[2]) {
+      constexpr int kMode = decltype(mode)::value;
+      // keys 0 .. upto - 1 of this lane's are seen: its keys are at steps of 1 and 8 from 4 half on
+      const int upto = limit <= pos ? 0 : limit - pos < 64 ? (int)(limit - pos) - 4 * (int)half : 64;
+      const Column col{limit, limit > a.window ? limit - a.window : 0, 0};
       score[0] = score[1] = f32x16{};
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        const u32x4 w = *(const lds_words*)(uintptr_t)(at ^ (i << 5));
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w), score[u], 0, 0, 0);
+          score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w[i]), score[u], 0, 0, 0);
+        if (i + 2 < kSteps) read(at, i + 2); else read(after, i + 2 - kSteps);
+#pragma unroll
+        for (int e = 32 / kSteps * i; e < 32 / kSteps * (i + 1); ++e) {
+          const int u = e / 16, r = e % 16, k = 32 * u + 8 * (r / 4) + r % 4;
+          const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(last[u][r], a.c, -l));
+          const bool in = kMode == 0 || (kMode == 1 ? k < upto : sees(col, pos + 4 * half + k, a.sinks));
+          acc[u][r] += in ? weight : 0.0f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // the weights of half c of tile m
-    const uint32_t half_row[2] = {quotient(lane & 31, a.group, a.group_magic),
-                                  quotient(32 + (lane & 31), a.group, a.group_magic)};
-    const auto weigh_some = [&](uint32_t m, int c, float lse, const f32x16 (&score)[2]) {
-      const float l = lse * kLog2e;
-      const int64_t i = (int64_t)m * rows + half_row[c], limit = before + i + 1;
-      Column col;
-      col.limit = fabsf(lse) < __builtin_inff() && half_row[c] < rows && i < it.n && limit > 0
-                      ? (uint32_t)(limit < 0xFFFFFFFF ? limit : 0xFFFFFFFF) : 0;
-      col.low = col.limit > a.window ? col.limit - a.window : 0;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t p = pos + 32 * u + 8 * (r / 4) + 4 * half + r % 4;
-          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(score[u][r], a.c, -l));
-          acc[u][r] += sees(col, p, a.sinks) ? w : 0.0f;
-        }
-    };
-    // scores of half c at `slot`, while the half before them becomes weights
-    const auto both = [&](uint32_t slot, int c, f32x16 (&score)[2], uint32_t m, float lse, bool full,
+    const auto both = [&](uint32_t at, uint32_t after, f32x16 (&score)[2], uint32_t m, int c, float lse, bool full,
                           const f32x16 (&last)[2]) {
-      if (full && __all(fabsf(lse) < __builtin_inff())) {
-        // two products, then what the vector unit does meanwhile; operands are read two
-        // steps ahead
-        const float l = half_row[1 - c] < rows ? lse * kLog2e : __builtin_inff();
-        uint32_t at = slot * F::kTile + 32 * c * D * 2 + lane_at;
-        asm volatile("" : "+v"(at));
-        score[0] = score[1] = f32x16{};
-        u32x4 w[kSteps];
-        const auto read = [&](int i) { w[i] = *(const lds_words*)(uintptr_t)(at ^ (i << 5)); };
-        read(0);
-        read(1);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          if (i + 2 < kSteps) read(i + 2);
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w[i]), score[u], 0, 0, 0);
-#pragma unroll
-          for (int e = 32 / kSteps * i; e < 32 / kSteps * (i + 1); ++e)
-            acc[e / 16][e % 16] += __builtin_amdgcn_exp2f(__builtin_fmaf(last[e / 16][e % 16], a.c, -l));
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      } else {
-        multiply(slot, c, score);
-        weigh_some(m, 1 - c, lse, last);
+      asm volatile("" : "+v"(at), "+v"(after));
+      const bool counts = fabsf(lse) < __builtin_inff();
+      const float l = half_row[c] < rows ? lse * kLog2e : __builtin_inff();
+      if (full && __all(counts)) {
+        step(std::integral_constant<int, 0>{}, at, after, score, l, 0, last);
+        return;
       }
+      const int64_t i = (int64_t)m * rows + half_row[c], limit = before + i + 1;
+      uint32_t sees_to = limit < 0xFFFFFFFF ? (uint32_t)limit : 0xFFFFFFFFu;
+      if (!counts || half_row[c] >= rows || i >= it.n || limit <= 0) sees_to = 0;
+      if (causal)
+        step(std::integral_constant<int, 1>{}, at, after, score, l, sees_to, last);
+      else
+        step(std::integral_constant<int, 2>{}, at, after, score, l, sees_to, last);
     };
     // this wave's tiles: some row sees some key in seen_from .. seen_to - 1, every row
     // every key in full_from .. full_to - 1
@@ -410,23 +402,33 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
     seen_to = uniform(seen_to);
     full_to = uniform(full_to);
     const auto seen = [&](uint32_t m) { return m >= seen_from && m < seen_to; };
-    uint32_t slot = 0;
-    f32x16 one[2], two[2];
+    // Half by half: (n - 1, 1) is weighed with the products of (n, 0), (n, 0) with those
+    // of (n, 1).  Tile n is there before it is needed: all waves meet, a tile ahead,
+    // when its copies have arrived and tile n - 2 has been read.
+    uint32_t slot = 0;  // tile n's
+    f32x16 one[2] = {}, two[2] = {};
+    float l1 = __builtin_inff();  // of the half before the first: it adds nothing
     wait_copies<2 * F::kCopies>();
     meet();
-    multiply(0, 0, one);
-    for (; n < end; ++n) {
-      const bool full = n >= full_from && n < full_to;
-      const float l0 = sums[slot][lane & 31], l1 = sums[slot][32 + (lane & 31)];
-      if (seen(n)) both(slot, 1, two, n, l0, full, one);
-      // tile n has been read, n + 1 is there
-      const uint32_t was = slot;
-      slot = slot == F::kRing - 1 ? 0 : slot + 1;
+    read(place(0, 0), 0);
+    read(place(0, 0), 1);
+    for (uint32_t m = n; m <= end; ++m) {
+      const uint32_t next = (slot + 1) % F::kRing;
       wait_copies<F::kCopies>();
       meet();
-      fetch(n + 3, was);
+      fetch(m + 3, (slot + 3) % F::kRing);
+      const float l0 = sums[slot][lane & 31];
       // (past the last: of columns that nobody weighs)
-      if (seen(n) || seen(n + 1)) both(slot, 0, one, n, l1, full, two);
+      if (seen(m) || (m > n && seen(m - 1)))
+        both(place(slot, 0), place(slot, 1), one, m - 1, 1, l1, m > n && m - 1 >= full_from && m - 1 < full_to, two);
+      if (m < end && seen(m)) {
+        both(place(slot, 1), place(next, 0), two, m, 0, l0, m >= full_from && m < full_to, one);
+      } else {
+        read(place(next, 0), 0);
+        read(place(next, 0), 1);
+      }
+      l1 = sums[slot][32 + (lane & 31)];
+      slot = next;
     }
     wait_loads();  // no copy outlives the workgroup
   }
