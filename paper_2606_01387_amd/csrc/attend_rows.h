@@ -82,23 +82,23 @@ struct WindowArgs : Args {
 template <bool WIN>
 using ArgsOf = std::conditional_t<WIN, WindowArgs, Args>;
 
-// Which keys of a tile a row sees: the first `hi`, and with a window those of them
-// from `lo` on or before `few`.
+// Which keys of a tile a row sees: the first `hi`, or with a window those of `bits`.
+// part(x): of the keys from x on.
 template <bool WIN>
 struct Seen {
   int hi;
-  __device__ __forceinline__ bool key(int x, int from = 0) const { return x < hi - from; }
+  __device__ __forceinline__ Seen part(int x) const { return {hi - x}; }
+  __device__ __forceinline__ bool key(int x) const { return x < hi; }
   __device__ __forceinline__ bool all(int keys) const { return !(hi < keys); }
 };
 
 template <>
 struct Seen<true> {
-  int hi, lo, few;
-  __device__ __forceinline__ bool key(int x, int from = 0) const {
-    return x < hi - from && (x >= lo - from || x < few - from);
-  }
-  __device__ __forceinline__ bool all(int keys) const { return hi >= keys && (lo <= 0 || few >= keys); }
-  __device__ __forceinline__ bool any() const { return hi > lo || (hi > 0 && few > 0); }
+  uint64_t bits;
+  __device__ __forceinline__ Seen part(int x) const { return {bits >> x}; }
+  __device__ __forceinline__ bool key(int x) const { return bits >> x & 1; }
+  static __device__ __forceinline__ uint64_t first(uint32_t n) { return n < 64 ? (1ull << n) - 1 : ~0ull; }
+  __device__ __forceinline__ bool all(int keys) const { return !(~bits & first(keys)); }
 };
 
 // A query row of this lane.
@@ -535,11 +535,12 @@ struct Wave {
   template <int U, bool WIN>
   __device__ __forceinline__ void mask(f32x16 (&s)[U], const Seen<WIN>& seen) const {
     const int h = (threadIdx.x >> 5) & 1;
+    const Seen<WIN> mine = seen.part(4 * h);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        s[u][r] = seen.key(32 * u + 8 * (r / 4) + r % 4, 4 * h) ? s[u][r] : kNoMax;
+        s[u][r] = mine.key(32 * u + 8 * (r / 4) + r % 4) ? s[u][r] : kNoMax;
   }
 
   // Weights of a tile, and the running maximum and sum.
@@ -614,14 +615,14 @@ struct Wave {
   // A whole tile of which the lane's row sees the keys `seen`.
   template <int U, bool WIN>
   __device__ __forceinline__ void tile(const Args& a, const uint8_t* lk, const uint8_t* lv,
-                                       const Seen<WIN>& seen) {
+                                       const Seen<WIN>& seen, bool bad = true) {
     f32x16 s[U];
     bf16x8 p[U][2];
     scores<U>(lk, s);
     const bool masked = __any(!seen.all(32 * U));
     if (masked) mask<U>(s, seen);
     weights<U>(a, s, p);
-    if (masked && nonfinite<U>(lv))
+    if (masked && bad && nonfinite<U>(lv))
       values_seen<U>(lv, p, seen);
     else
       values<U>(lv, p);
@@ -629,16 +630,19 @@ struct Wave {
 
   // Whether the tile of V holds an infinity or a NaN: a weight of 0 does not
   // take it out of the product.
+  static __device__ __forceinline__ bool nonfinite(u32x4 w) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+    return bad;
+  }
+
   template <int U>
   __device__ __forceinline__ bool nonfinite(const uint8_t* lv) const {
     bool bad = false;
 #pragma unroll 1
-    for (uint32_t at = (threadIdx.x & 63) * 16; at < 32 * U * D * 2; at += 1024) {
-      const u32x4 w = *(const u32x4*)(lv + at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
-    }
+    for (uint32_t at = (threadIdx.x & 63) * 16; at < 32 * U * D * 2; at += 1024)
+      bad |= nonfinite(*(const u32x4*)(lv + at));
     return __any(bad);
   }
 
@@ -964,15 +968,15 @@ __device__ __forceinline__ void hold(bf16x8 (&p)[2][2]) {
 // Which of the `keys` positions from `pos` on the row sees.
 template <bool WIN>
 __device__ __forceinline__ Seen<WIN> seen_of(const ArgsOf<WIN>& a, const Row& r, uint32_t pos, uint32_t keys) {
-  const auto upto = [&](uint32_t end) { return end <= pos ? 0 : end - pos < keys ? (int)(end - pos) : (int)keys; };
-  Seen<WIN> s;
-  s.hi = upto(r.limit);
+  const auto upto = [&](uint32_t end) { return end <= pos ? 0 : end - pos < keys ? end - pos : keys; };
   if constexpr (WIN) {
-    const uint32_t low = r.limit > a.window ? r.limit - a.window : 0;
-    s.lo = upto(low < a.room ? low : a.room);
-    s.few = upto(a.sinks);
+    uint32_t low = r.limit > a.window ? r.limit - a.window : 0;
+    low = low < a.room ? low : a.room;
+    const auto below = [&](uint32_t end) { return Seen<true>::first(upto(end)); };
+    return {below(r.limit) & (~below(low) | below(a.sinks))};
+  } else {
+    return {(int)upto(r.limit)};
   }
-  return s;
 }
 
 // ----------------------------------------------------------- many query rows
@@ -1008,11 +1012,15 @@ struct Many {
     __align__(1024) uint8_t v[(kAhead + 1) * kTile];
     uint32_t least[WAVES];
   };
+  struct WithBad : Lds {
+    uint32_t bad[2][WAVES];  // what of a tile of V each wave brought holds an infinity or a NaN
+  };
 };
 
 template <int D, bool E4M3, int WAVES, Within WITHIN, bool WIN = false>
 __device__ __forceinline__ void many_rows(const ArgsOf<WIN>& a, bool prefix, uint32_t b,
-                                          typename Many<D, WAVES>::Lds& shared) {
+                                          std::conditional_t<WIN, typename Many<D, WAVES>::WithBad,
+                                                             typename Many<D, WAVES>::Lds>& shared) {
   using F = Many<D, WAVES>;
   constexpr int M = WAVES * 32, kKeys = F::kKeys, kTile = F::kTile, kAhead = F::kAhead;
   using St = Stage<D * (E4M3 ? 1 : 2), E4M3, kKeys, WAVES * 64, WITHIN, WideSwizzle<D>>;
@@ -1142,17 +1150,46 @@ __device__ __forceinline__ void many_rows(const ArgsOf<WIN>& a, bool prefix, uin
     meet();
   }
   if constexpr (WIN) {
+    // A window has more tiles with a mask than a diagonal has: each wave looks through
+    // what it brought of V itself, and copies are waited for a tile after they began.
+    const auto look = [&](uint32_t tile, uint32_t at) {  // tile `tile` of V, at `at` in the ring
+      bool bad = false;
+      if (E4M3) {  // a thread's own row, as land() wrote it
+#pragma unroll
+        for (int i = 0; i < St::kSteps; ++i) {
+          const uint32_t row = i * St::kRows + t / St::kRowLanes, chunk = 2 * (t % St::kRowLanes);
+          if (kKeys < St::kRows && row >= kKeys) break;
+          const uint8_t* of = lv + at + row * D * 2;
+          bad |= w.nonfinite(*(const u32x4*)(of + (chunk ^ WideSwizzle<D>::v(row)) * 16)) ||
+                 w.nonfinite(*(const u32x4*)(of + ((chunk + 1) ^ WideSwizzle<D>::v(row)) * 16));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < St::kSteps; ++i) bad |= w.nonfinite(*(const u32x4*)(lv + at + i * WAVES * 1024 + t * 16));
+      }
+      if (__any(bad) && (t & 63) == 0) shared.bad[tile & 1][t >> 6] = 1;
+      if (!__any(bad) && (t & 63) == 0) shared.bad[tile & 1][t >> 6] = 0;
+    };
+    if (n < it.walk.count) {
+      look(n, now);
+      meet();
+    }
 #pragma unroll 1
     for (; n < it.walk.count;) {
       const bool more = n + 1 < it.walk.count;
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) bad |= shared.bad[n & 1][i];
       if (more) fetch();
       const auto seen = seen_of<true>(a, row, walk_pos<kKeys>(it.walk, n), kKeys);
-      if (__any(seen.any())) w.template tile<2, true>(a, lk + now, lv + now, seen);
+      if (__any(seen.bits != 0)) w.template tile<2, true>(a, lk + now, lv + now, seen, uniform(bad));
       if (!more) break;
       step();
-      wait_loads();
+      if (!E4M3) wait_copies<2 * St::kSteps>();
+      look(n, now);
       meet();
     }
+    wait_loads();  // the copies of tiles past the last
   } else {
 #pragma unroll 1
     for (uint32_t pos = lo + full * kKeys; pos < hi; pos += kKeys) {  // hi + kKeys fits 32 bits
@@ -1277,7 +1314,7 @@ struct Narrow {
       for (int n = 0; n < kSub; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          if (masked) s[c][n][r] = seen[c].key(16 * n + r, g4) ? s[c][n][r] : kNoMax;
+          if (masked) s[c][n][r] = seen[c].part(g4).key(16 * n + r) ? s[c][n][r] : kNoMax;
           x = fmaxf(x, s[c][n][r]);
         }
       const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -1520,7 +1557,10 @@ __device__ __forceinline__ void few_rows(
       Seen<WIN> seen[QT];
 #pragma unroll
       for (int c = 0; c < QT; ++c) {
-        seen[c] = {kKeys};
+        if constexpr (WIN)
+          seen[c] = {Seen<true>::first(kKeys)};
+        else
+          seen[c] = {kKeys};
         if (masked) seen[c] = seen_of<WIN>(a, row[c], WIN ? walk_pos<kKeys>(it.walk, pos) : pos, kKeys);
       }
       at = st.place(a, rows, rest(pos + 2 * kMore));

@@ -14,7 +14,7 @@ namespace {
 
 template <int D, bool E4M3, Within WITHIN>
 __global__ void __launch_bounds__(512, 2) k_window_rows(WindowArgs a) {
-  __shared__ typename Many<D, 8>::Lds shared;
+  __shared__ typename Many<D, 8>::WithBad shared;
   many_rows<D, E4M3, 8, WITHIN, true>(a, false, blockIdx.x, shared);
 }
 
