@@ -50,9 +50,45 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The k-th largest (k >= 1) of the weights at lo .. hi - 1, by the numbers' digits
-// from the highest on; *equal is how many of that very number are among the k.
-__device__ uint32_t kth_largest(const float* w, uint32_t lo, uint32_t hi, uint32_t k, uint32_t* equal) {
+// A thread's weights as numbers: wave w has a run of positions, its lanes the run's
+// 64 at a time.  The first of them stay in registers from one look to the next.
+constexpr uint32_t kNear = 8;
+
+struct Numbers {
+  const float* w;
+  uint32_t begin, end, run;  // the wave's positions; run: a multiple of 64
+  uint32_t near[kNear];
+
+  __device__ __forceinline__ void start(const float* weights, uint32_t len) {
+    w = weights;
+    run = (len / kPlan + 1) * 64;
+    begin = threadIdx.x / 64 * run;
+    begin = begin < len ? begin : len;
+    end = len - begin < run ? len : begin + run;
+    float x[kNear];  // all of them on their way at once
+#pragma unroll
+    for (uint32_t k = 0; k < kNear; ++k) {
+      const uint32_t p = begin + 64 * k + threadIdx.x % 64;
+      x[k] = p < end && 64 * k < run ? w[p] : 0.0f;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kNear; ++k) near[k] = order_of(x[k]);
+  }
+
+  // f(position, number) for each 64 positions of the wave, all lanes together.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    const uint32_t lane = threadIdx.x % 64;
+#pragma unroll
+    for (uint32_t k = 0; k < kNear; ++k)
+      if (begin + 64 * k < end) f(begin + 64 * k + lane, near[k]);
+    for (uint32_t p = begin + 64 * kNear; p < end; p += 64) f(p + lane, p + lane < end ? order_of(w[p + lane]) : 0);
+  }
+};
+
+// The k-th largest (k >= 1) of the numbers at lo .. hi - 1, by their digits from the
+// highest on; *equal is how many of that very number are among the k.
+__device__ uint32_t kth_largest(const Numbers& numbers, uint32_t lo, uint32_t hi, uint32_t k, uint32_t* equal) {
   __shared__ uint32_t count[2048];
   __shared__ uint32_t found, left;
   const uint32_t t = threadIdx.x;
@@ -61,10 +97,9 @@ __device__ uint32_t kth_largest(const float* w, uint32_t lo, uint32_t hi, uint32
     const uint32_t shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
     count[t] = count[t + kPlan] = 0;
     __syncthreads();
-    for (uint32_t p = lo + t; p < hi; p += kPlan) {
-      const uint32_t x = order_of(w[p]);
-      if ((x & mask) == prefix) atomicAdd(&count[x >> shift & (bins - 1)], 1u);
-    }
+    numbers.each([&](uint32_t p, uint32_t x) {
+      if (p >= lo && p < hi && (x & mask) == prefix) atomicAdd(&count[x >> shift & (bins - 1)], 1u);
+    });
     __syncthreads();
     // thread t has the bins bins - 1 - 2 t and the one below
     const uint32_t a = 2 * t < bins ? count[bins - 1 - 2 * t] : 0, b = 2 * t < bins ? count[bins - 2 - 2 * t] : 0;
@@ -87,7 +122,8 @@ __device__ uint32_t kth_largest(const float* w, uint32_t lo, uint32_t hi, uint32
 
 // A workgroup chooses what an entry keeps: the weights above the last that has a
 // place, and of those equal to it the first ones.  Waves take runs of positions,
-// count, and then write what they keep in order.
+// count, and then write what they keep in order.  Bound by dependent reads (length,
+// table and weights, counts) and the digits' barriers.
 __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
   __shared__ uint32_t above[kPlan / 64], same[kPlan / 64], gone;
   const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -99,6 +135,9 @@ __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
     const uint32_t len = r < a.s.max_seqs ? a.s.lengths[r] : 0;
     const uint32_t held = len / a.bs + (len % a.bs != 0);
     bad |= held > a.s.max_blocks;
+    const bool cut = !bad && len > a.tokens;
+    Numbers numbers;
+    numbers.start(a.weights + (r < a.s.max_seqs ? r : 0) * a.weights_row, cut ? len : 0);
     uint32_t* from = a.from + (uint64_t)i * a.s.max_blocks;
     if (!bad)
       for (uint32_t j = t; j < held; j += kPlan) {
@@ -113,24 +152,18 @@ __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
       if (t == 0) a.entries[i] = Entry{bad ? kRefused : kShort, len, 0, 0, 0, 0, {}};
       continue;
     }
-    const float* w = a.weights + r * a.weights_row;
     const uint32_t lo = a.sinks, hi = len - a.recent, m = a.tokens - a.sinks - a.recent;
     uint32_t least = ~0u, equal = 0;  // (no weight has the highest number)
-    if (m) least = kth_largest(w, lo, hi, m, &equal);
-    const uint32_t run = (len / kPlan + 1) * 64;  // positions of a wave
-    const uint32_t begin = wave * run < len ? wave * run : len, end = len - begin < run ? len : begin + run;
-    const auto kind = [&](uint32_t p) {  // 0: goes, 1: equal to the least, 2: stays
-      if (p >= end) return 0;
-      if (p < lo || p >= hi) return 2;
-      const uint32_t x = order_of(w[p]);
-      return x > least ? 2 : x == least ? 1 : 0;
+    if (m) least = kth_largest(numbers, lo, hi, m, &equal);
+    const auto kind = [&](uint32_t p, uint32_t x) {  // 0: goes, 1: equal to the least, 2: stays
+      return p >= numbers.end ? 0 : p < lo || p >= hi || x > least ? 2 : x == least ? 1 : 0;
     };
     uint32_t more = 0, ties = 0;
-    for (uint32_t p = begin; p < end; p += 64) {
-      const int x = kind(p + lane);
+    numbers.each([&](uint32_t p, uint32_t number) {
+      const int x = kind(p, number);
       more += __popcll(__ballot(x == 2));
       ties += __popcll(__ballot(x == 1));
-    }
+    });
     if (lane == 0) {
       above[wave] = more;
       same[wave] = ties;
@@ -145,16 +178,16 @@ __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
     at += tied < equal ? tied : equal;
     const uint64_t below = (1ull << lane) - 1;
     uint32_t mine = len;  // the first position that goes
-    for (uint32_t p = begin; p < end; p += 64) {
-      const int x = kind(p + lane);
+    numbers.each([&](uint32_t p, uint32_t number) {
+      const int x = kind(p, number);
       const uint64_t t1 = __ballot(x == 1);
       const bool stays = x == 2 || (x == 1 && tied + __popcll(t1 & below) < equal);
       const uint64_t k1 = __ballot(stays);
-      if (stays) kept[at + __popcll(k1 & below)] = p + lane;
-      if (!stays && p + lane < end && p + lane < mine) mine = p + lane;
+      if (stays) kept[at + __popcll(k1 & below)] = p;
+      if (!stays && p < numbers.end && p < mine) mine = p;
       at += __popcll(k1);
       tied += __popcll(t1);
-    }
+    });
     if (mine < len) atomicMin(&gone, mine);
     __syncthreads();
     const uint32_t stay = gone < a.tokens ? gone : a.tokens;

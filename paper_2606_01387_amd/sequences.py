@@ -180,41 +180,36 @@ class Sequences:
         and ``k_norm`` (bf16 [head_dim]) are the weights of x w / sqrt(mean(x^2)
         + eps); None leaves heads as they are."""
         pool, shape = self.pool, q.shape
-        if len(shape) != 3 or k.shape[0] != shape[0] or v.shape[0] != shape[0]:
-            raise ValueError("q must be [rows, heads, head_dim], and k and v have the same rows")
-        rows, heads = shape[0], shape[1]
-        given = (*self._rows("q", q, heads), *self._rows("k", k, self._heads),
-                 *self._rows("v", v, self._heads))
+        if len(shape) != 3:
+            raise ValueError("q must be [rows, heads, head_dim]")
+        rows, heads, _ = shape
+        given = (*self._rows("q", q, heads), *self._rows("k", k, self._heads, rows),
+                 *self._rows("v", v, self._heads, rows))
         if out is None:
             out = q.new_empty(shape)
         elif out.shape != shape:
             raise ValueError("out needs q's shape")
-        pairs = 0 if freqs is None else freqs.numel()
-        if pairs and (freqs.dtype != self._float64 or freqs.device != self._device
-                      or not freqs.is_contiguous()):
-            raise ValueError(f"freqs must be a contiguous float64 tensor on {self._device}")
+        freqs_at = pairs = 0
+        if freqs is not None:
+            freqs_at, pairs = freqs.data_ptr(), freqs.numel()
+            if freqs.dtype != self._float64 or freqs.device != self._device or not freqs.is_contiguous():
+                raise ValueError(f"freqs must be a contiguous float64 tensor on {self._device}")
         sections = (pairs,) if sections is None else tuple(sections)
-        at, row_stride, axis_stride = 0, 0, 0
+        at = row_stride = axis_stride = 0
         if positions is not None:
-            axes = positions.shape[1] if positions.dim() == 2 else 1
+            given_as, strides = positions.shape, positions.stride()
             if (positions.dtype != self._int32 or positions.device != self._device
-                    or positions.dim() not in (1, 2) or positions.shape[0] != rows):
+                    or len(given_as) not in (1, 2) or given_as[0] != rows):
                 raise ValueError(f"positions must be int32 [rows] or [rows, axes] on {self._device}")
-            if axes != len(sections):
+            if (given_as[1] if len(given_as) == 2 else 1) != len(sections):
                 raise ValueError("positions need as many axes as sections")
-            at, row_stride = positions.data_ptr(), positions.stride(0)
-            axis_stride = positions.stride(1) if positions.dim() == 2 else 0
+            at, row_stride, axis_stride = positions.data_ptr(), strides[0], strides[1] if len(strides) == 2 else 0
         if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != pairs:
             raise ValueError("sections must be up to 4 numbers of pairs that add up to freqs'")
-        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-            if w is not None and (w.dtype != self._bf16 or w.device != self._device
-                                  or w.numel() != self._dim or not w.is_contiguous()):
-                raise ValueError(f"{name} must be contiguous bf16 [{self._dim}] on {self._device}")
         _ROTATE.pack_into(self._desc, 0, *self._kv(layer, rows, ids, offsets), k_scale, v_scale, *given,
-                          *self._rows("out", out, heads), heads, 2 * pairs,
-                          freqs.data_ptr() if pairs else 0, at, row_stride, axis_stride,
-                          *(sections + (0, 0, 0))[:4], 0 if q_norm is None else q_norm.data_ptr(),
-                          0 if k_norm is None else k_norm.data_ptr(), eps, 1 if neighbours else 0)
+                          *self._rows("out", out, heads), heads, 2 * pairs, freqs_at, at, row_stride,
+                          axis_stride, *(sections + (0, 0, 0))[:4], self._norm("q_norm", q_norm),
+                          self._norm("k_norm", k_norm), eps, 1 if neighbours else 0)
         with pool.ordered(self, q, k, v, out, freqs, positions, q_norm, k_norm, ids, offsets):
             _check(self._lib.claim_kv_write_rotated(pool._h, self._seqs_ref, self._desc_at),
                    "claim_kv_write_rotated")
@@ -363,12 +358,22 @@ class Sequences:
             raise ValueError("offsets needs one entry more than sequences; layer must not be negative")
         return layer, n, rows, 0, ids_at, offsets_at
 
-    def _rows(self, name, x, heads):
+    def _norm(self, name, w) -> int:
+        """The address of a head's weights, or 0."""
+        if w is None:
+            return 0
+        if w.dtype != self._bf16 or w.device != self._device or w.numel() != self._dim or not w.is_contiguous():
+            raise ValueError(f"{name} must be contiguous bf16 [{self._dim}] on {self._device}")
+        return w.data_ptr()
+
+    def _rows(self, name, x, heads, rows=None):
         """claim_rows."""
-        stride, dim = x.stride(), self._dim
+        stride, shape = x.stride(), x.shape
         if (x.dtype != self._bf16 or x.device != self._device or len(stride) != 3
-                or x.shape[1] != heads or x.shape[2] != dim or stride[2] != 1):
-            raise ValueError(f"{name} must be bf16 [rows, {heads}, {dim}] on {self._device}, "
+                or shape[1] != heads or shape[2] != self._dim or stride[2] != 1):
+            raise ValueError(f"{name} must be bf16 [rows, {heads}, {self._dim}] on {self._device}, "
                              "its last dimension contiguous")
+        if rows is not None and shape[0] != rows:
+            raise ValueError(f"{name} needs {rows} rows")
         # the stride of a single row or head leads nowhere, and may be anything
-        return x.data_ptr(), stride[0] if x.shape[0] > 1 else 0, stride[1] if heads > 1 else 0
+        return x.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if heads > 1 else 0
