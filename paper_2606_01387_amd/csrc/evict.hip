@@ -120,6 +120,23 @@ __device__ uint32_t kth_largest(const Numbers& numbers, uint32_t lo, uint32_t hi
   return prefix;
 }
 
+// Whether an earlier entry names the same row: each workgroup looks through the
+// entries before its own where they are few, else two launches have left the first
+// entry of every row in `owner` (a look through n entries by n workgroups takes n^2).
+constexpr uint32_t kLookThrough = 4096;
+
+__global__ void __launch_bounds__(256) k_owner_none(uint32_t* owner, const uint32_t* ids, uint32_t n,
+                                                    uint32_t max_seqs) {
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256)
+    if (ids[i] < max_seqs) owner[ids[i]] = kNone;
+}
+
+__global__ void __launch_bounds__(256) k_owner_first(uint32_t* owner, const uint32_t* ids, uint32_t n,
+                                                     uint32_t max_seqs) {
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256)
+    if (ids[i] < max_seqs) atomicMin(&owner[ids[i]], i);
+}
+
 // A workgroup chooses what an entry keeps: the weights above the last that has a
 // place, and of those equal to it the first ones.  Waves take runs of positions,
 // count, and then write what they keep in order.  Bound by dependent reads (length,
@@ -130,8 +147,12 @@ __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
   for (uint32_t i = blockIdx.x; i < a.n; i += gridDim.x) {
     const uint32_t r = row_of(a.ids, i);
     bool bad = r >= a.s.max_seqs;
-    if (a.ids && !bad)
-      for (uint32_t k = t; k < i; k += kPlan) bad |= a.ids[k] == r;
+    if (a.ids && !bad) {
+      if (a.n > kLookThrough)
+        bad = a.s.owner[r] != i;
+      else
+        for (uint32_t k = t; k < i; k += kPlan) bad |= a.ids[k] == r;
+    }
     const uint32_t len = r < a.s.max_seqs ? a.s.lengths[r] : 0;
     const uint32_t held = len / a.bs + (len % a.bs != 0);
     bad |= held > a.s.max_blocks;
@@ -404,6 +425,11 @@ int claim_seqs_evict(claim_pool* P, const claim_seqs* s, const claim_evict_desc*
   while (a.width > 16 && (uint64_t)d->n * a.planes * ((a.token_units + a.width - 1) / a.width) < 4ull * p.cus) a.width /= 2;
   a.slices = (a.token_units + a.width - 1) / a.width;
   SEQ_HIP(hipSetDevice(p.device));
+  if (d->ids && d->n > kLookThrough) {
+    const dim3 some(4 * p.cus);
+    hipLaunchKernelGGL(k_owner_none, some, dim3(256), 0, p.stream, a.s.owner, d->ids, d->n, s->max_seqs);
+    hipLaunchKernelGGL(k_owner_first, some, dim3(256), 0, p.stream, a.s.owner, d->ids, d->n, s->max_seqs);
+  }
   hipLaunchKernelGGL(k_evict_select, dim3(d->n < 65536 ? d->n : 65536), dim3(kPlan), 0, p.stream, a);
   hipLaunchKernelGGL(k_evict_plan, dim3(1), dim3(kPlan), 0, p.stream, a);
   const uint64_t items = (uint64_t)d->n * (a.planes * (uint64_t)a.slices + 1), most = 16ull * p.cus;

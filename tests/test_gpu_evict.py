@@ -244,6 +244,18 @@ def test_many_entries(torch, ck):
         p.evict(list(range(1400, 300, -1)), 5)
 
 
+def test_entries_past_what_a_workgroup_looks_through(torch, ck):
+    """Thousands of entries, some rows named again by later ones."""
+    n = 6000
+    p = Evicting(torch, ck, n, 2, geometry(2 * n + 64, 4, 1, 8, 1, 1, 1), seed=14)
+    with p.pool:
+        p.do("grow", list(range(5900)), [7 if i % 2 else 3 for i in range(5900)])
+        p.do("fork", [1, 3, 5], [5900, 5901, 5902])
+        ids = list(range(5999, 0, -1))
+        ids[4500], ids[5000], ids[5500] = 5999 - 17, 5901, -1
+        p.evict(ids, 5, 1, 1)
+
+
 def test_identities(torch, ck):
     """A rewritten block gives up the prefix that it held; those before it and
     claims' held blocks keep theirs."""
