@@ -58,25 +58,40 @@ __device__ __forceinline__ u32x4 narrow(const Eight& e) {
   return __builtin_bit_cast(u32x4, b);
 }
 
-// A head's weights: this lane's, and those of the elements its own turn with, as
-// they are in memory: widened where they are used, they take 16 registers less.
-struct Weights {
-  u32x4 own, other;
-};
-
-__device__ __forceinline__ Weights weights(const uint16_t* norm, uint32_t at, uint32_t other) {
+// A head's weights at this lane's elements, as they are in memory: widened where they
+// are used, they take fewer registers.
+__device__ __forceinline__ u32x4 weights(const uint16_t* norm, uint32_t at) {
   constexpr uint32_t kOnes = 0x3F803F80u;
-  Weights w{{kOnes, kOnes, kOnes, kOnes}, {kOnes, kOnes, kOnes, kOnes}};
-  if (norm) {
-    w.own = *(const u32x4*)(norm + at);
-    w.other = *(const u32x4*)(norm + other);
-  }
-  return w;
+  return norm ? *(const u32x4*)(norm + at) : u32x4{kOnes, kOnes, kOnes, kOnes};
+}
+
+// The value of the lane that a rule within rows of 16 lanes names; lanes of the banks
+// (of 4) that `BANKS` leaves out keep `old`.
+template <int RULE, int BANKS = 15>
+__device__ __forceinline__ float lane_rule(float x, float old = 0.0f) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(old), __float_as_uint(x), RULE, 15, BANKS, false));
+}
+
+// A value's sum over the LANES (8 or 16) of a head, on all of them.
+template <uint32_t LANES>
+__device__ __forceinline__ float sum_head(float x) {
+  x += lane_rule<0xB1>(x);   // lane ^ 1
+  x += lane_rule<0x4E>(x);   // lane ^ 2
+  x += lane_rule<0x141>(x);  // 7 - lane of eight
+  return LANES == 16 ? x + lane_rule<0x140>(x) : x;  // 15 - lane of sixteen
+}
+
+// The value of the head's lane half of its lanes on.
+template <uint32_t LANES>
+__device__ __forceinline__ float across_head(float x) {
+  if (LANES == 16) return lane_rule<0x128>(x);             // eight lanes round
+  return lane_rule<0x104, 5>(x, lane_rule<0x114, 10>(x));  // four lanes up, four down
 }
 
 // A wave takes a row, or a part of its heads where rows are few; D / 8 lanes hold
 // a head, 8 neighbouring elements each.  A pair's other element is in the same
-// lane (NEIGHBOURS), or rot / 2 elements on, in another lane of the head.  The
+// lane (NEIGHBOURS), or rot / 2 elements on, in another lane of the head (where
+// all of it turns half of its lanes on, which takes no way through LDS).  The
 // loads of the first heads are on their way while the row's place, position
 // and angles (one pair a lane, then LDS) are looked up.
 template <int D, bool E4M3, bool NEIGHBOURS>
@@ -92,12 +107,9 @@ __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
   uint64_t token = 0;
   float c[8], n[8];  // cosines and sines of this lane's elements, signed
   const bool turned = at < 2 * a.half;
-  uint32_t other = at, other_lane = lane;
-  if (!NEIGHBOURS && turned) {
-    other = at < a.half ? at + a.half : at - a.half;
-    other_lane = lane - at / 8 + other / 8;
-  }
-  Weights qw, kw;
+  const bool whole = !NEIGHBOURS && 2 * a.half == D;
+  const uint32_t other_lane = NEIGHBOURS || !turned ? lane : at < a.half ? lane + a.half / 8 : lane - a.half / 8;
+  u32x4 qw, kw;
   for (uint32_t h0 = part * kHeads; h0 < heads; h0 += a.waves * kHeads * kMany) {
     u32x4 w[kMany];
 #pragma unroll
@@ -111,8 +123,8 @@ __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
       w[j] = *(const u32x4*)(from + at);
     }
     if (h0 == part * kHeads) {
-      qw = weights(a.q_norm, at, other);
-      kw = weights(a.k_norm, at, other);
+      qw = weights(a.q_norm, at);
+      kw = weights(a.k_norm, at);
       uint32_t r = 0;
       int64_t pos = 0;
       there = row_position(a, s, row, &r, &pos);
@@ -149,33 +161,28 @@ __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
       const uint32_t h = h0 + j * a.waves * kHeads + lane / kLanes;
       const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.kv_heads;
       const u32x4 mine = w[j];
-      u32x4 theirs = mine;
-      if (!NEIGHBOURS)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) theirs[i] = __shfl(mine[i], other_lane);
-      const Eight y = widen(mine), z = widen(theirs);
-      float square = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) square = __builtin_fmaf(y.x[i], y.x[i], square);
-#pragma unroll
-      for (uint32_t d = 1; d < kLanes; d <<= 1) square += __shfl_xor(square, d);
-      if (h >= heads) continue;
-      const float f = (is_q ? a.q_norm : a.k_norm) ? rsqrtf(square * (1.0f / D) + a.eps) : 1.0f;
+      const Eight y = widen(mine);
       Eight o = y;
-      if (!is_v) {
+      if (__any(!is_v)) {
+        float square = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) square = __builtin_fmaf(y.x[i], y.x[i], square);
+        square = sum_head<kLanes>(square);
+        const float f = (is_q ? a.q_norm : a.k_norm) ? rsqrtf(square * (1.0f / D) + a.eps) : 1.0f;
+        const Eight own = widen(is_q ? qw : kw);
         Eight p, r;
-        const Eight own = widen(is_q ? qw.own : kw.own), others = widen(is_q ? qw.other : kw.other);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.x[i] = y.x[i] * f * own.x[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          r.x[i] = NEIGHBOURS ? p.x[i ^ 1] : whole ? across_head<kLanes>(p.x[i]) : __shfl(p.x[i], other_lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p.x[i] = y.x[i] * f * own.x[i];
-          r.x[i] = z.x[i] * f * others.x[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float partner = NEIGHBOURS ? p.x[i ^ 1] : r.x[i];
-          o.x[i] = turned ? __builtin_fmaf(p.x[i], c[i], partner * n[i]) : p.x[i];
+          const float z = turned ? __builtin_fmaf(p.x[i], c[i], r.x[i] * n[i]) : p.x[i];
+          o.x[i] = is_v ? y.x[i] : z;
         }
       }
+      if (h >= heads) continue;
       if (is_q) {
         *(u32x4*)(a.out + row * a.out_row + h * a.out_head + at) = narrow(o);
       } else if (held) {
