@@ -42,7 +42,10 @@
  * calls at the end of this file: claim_seqs_grow, claim_seqs_fork,
  * claim_seqs_free and claim_seqs_compact hand blocks out, share, take back and
  * move them, claim_blocks_copy copies them, claim_kv_write fills them and
- * claim_attend reads them.
+ * claim_attend reads them.  A program that bounds its sequences' caches norms and
+ * turns keys on their way in (claim_kv_write_rotated), attends in a window
+ * (claim_attend_window), adds up what each cached token weighed (claim_weigh) and
+ * cuts sequences to the tokens that weighed most (claim_seqs_evict).
  *
  * The digest, keys and chain are this library's definitions (the paper
  * leaves the byte-level check open; section 7 path B only requires

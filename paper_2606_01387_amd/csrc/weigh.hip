@@ -131,9 +131,10 @@ __device__ __forceinline__ float sum16(float x) {
 // or one); their sums meet in LDS.  Bound by memory: each key is read once, for
 // all heads of its group.  A lane has key lane % 16 of 16 and, of each 32
 // elements, eight; keys and queries take them in the same order.  64 sequences of up
-// to 8192 tokens, 8 KV heads of 128 for 4 query heads each, in 122 us, 5.0 TB/s; with
-// half of the keys on their way while the other half is weighed, in twice the
-// registers, 131 us.
+// to 8192 tokens, 8 KV heads of 128 for 4 query heads each, in 126 us, 4.9 TB/s.  Half
+// of the keys on their way while the other half is weighed takes more registers and
+// 134 us; what is left is the order of the loads, 64 bytes of 16 keys each: whole keys
+// one after another would take 118 us, but not lie as the products need them.
 
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
@@ -230,9 +231,16 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 // Four waves of 64 keys each of one KV head take a chunk of the sequence's columns,
 // 64 at a time through LDS, in two halves: while one half's scores become weights on
 // the vector unit, the matrix cores make those of the next.  A ring of four tiles:
-// two are on their way while one is read and one is there.  A tile is as many whole rows as 64 columns
-// hold (63 columns of a group of 7), so that a lane's place in it is the same in
-// every tile.
+// two are on their way while one is read and one is there.  A tile is as many whole
+// rows as 64 columns hold (63 columns of a group of 7), so that a lane's place in it
+// is the same in every tile.
+//
+// Bound by both units at once: 16 products and 96 vector operations of a wave take
+// 0.38 us together on a SIMD, 0.28 and 0.25 us alone.  8192 causal rows of 32 query
+// heads over 8 of 128 take 312 to 321 us (0.86 to 0.88 PFLOP/s of the pairs that are
+// seen), of which reading operands from LDS is some 50, copies to LDS 35, the masks on the
+// diagonal 15 and the beginnings of 2048 workgroups 20.  Eight waves to a workgroup:
+// 361 us; half or twice the chunks: 404 and 343 us; one phase after the other: 478 us.
 
 constexpr uint32_t kManyWaves = 4, kManyKeys = 64 * kManyWaves, kManyColumns = 64;
 
