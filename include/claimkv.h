@@ -704,7 +704,8 @@ int claim_attend(claim_pool* pool, const claim_seqs* seqs, const claim_attend_de
  * window + 1 .. P and the first ones, 0 .. sinks - 1 (those up to P).  Only blocks
  * of positions that some row sees are read: entries behind the window may be
  * CLAIM_NONE.  window is at least 1 (2^32 - 1: all positions), prefix_blocks 0 and
- * prefix NULL; everything else is as claim_attend has it.
+ * prefix NULL; everything else is as claim_attend has it.  Rows behind the last
+ * sequence (a padded batch: offsets that end before num_rows) are left as they were.
  *
  * With lse (float [num_rows][num_heads], may be NULL) each row's and head's
  * logarithm of sum_p exp(scale * k_scale * q . k_p) is written there, for
@@ -730,6 +731,8 @@ int claim_attend_window(claim_pool* pool, const claim_seqs* seqs, const claim_wi
  * lse.  A row and head whose lse is not finite adds nothing.  Weights, sums and lse
  * are in 32 bits, and equal bits on every run, but for a sequence named twice, which
  * gets both sums in either order.  Other entries of weights stay as they are.
+ * claim_seqs_fork does not copy a row of weights, and claim_seqs_free does not clear
+ * it: that is the program's to do before the row is used again.
  *
  * weights_stride is at least max_blocks * block_size; limits as for claim_attend, and
  * max_blocks * block_size below 2^31.  work: claim_weigh_work bytes, 256-byte aligned

@@ -1687,6 +1687,8 @@ __global__ void __launch_bounds__(256) k_join(ArgsOf<WIN> a) {
   const uint32_t x = blockIdx.x * 4 + uniform(threadIdx.x >> 6);
   const uint32_t lane = threadIdx.x & 63;
   if (x >= a.rows * heads) return;
+  if constexpr (WIN)  // rows before the first sequence and behind the last have no parts
+    if (a.offsets && (x / heads < a.offsets[0] || x / heads >= a.offsets[a.num_seqs])) return;
   const float2* ml = a.part_ml + (uint64_t)x * splits;
   float2 p[2];
 #pragma unroll

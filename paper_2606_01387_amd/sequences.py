@@ -255,7 +255,8 @@ class Sequences:
         column for every position that a table has) what each cached token weighed
         for the rows of ``q``, whose logarithms ``lse`` :meth:`attend_window` gave
         with the same window, sinks and scales.  ``q`` and ``lse`` may be a
-        prompt's last rows alone."""
+        prompt's last rows alone.  :meth:`fork` does not copy a row of weights,
+        and :meth:`free` does not clear it."""
         shape = q.shape
         if len(shape) != 3:
             raise ValueError("q must be [rows, heads, head_dim]")

@@ -98,6 +98,27 @@ def test_sequences_without_rows_or_length(torch, ck):
     both(ck, w)
 
 
+@pytest.mark.parametrize("seqs", [[(1, 60), (2, 9)], [(90, 30), (5, 0)], [(1, 3000)], [(200, 2500)]], ids=str)
+def test_rows_behind_the_last_sequence_are_left(torch, ck, seqs):
+    """A padded batch, with parts to join and without."""
+    w = WindowWorld(torch, seqs=seqs, heads=1, group=4, window=2000, sinks=2, seed=17)
+    want, bound, lse, room = w.expected()
+    pool, s, d = w.to_gpu(ck)
+    out = torch.full((w.rows + 9, 4, w.dim), 5.0, dtype=torch.bfloat16, device="cuda")
+    sums = torch.full((w.rows + 9, 4), 5.0, device="cuda")
+    with pool:
+        q = torch.cat([d.q, torch.full_like(out[:9], float("nan"))])
+        s.attend_window(w.layer, q, w.window, sinks=w.sinks, offsets=d.offsets, lse=sums, out=out)
+        weights = torch.zeros(len(seqs), w.tables.shape[1] * w.bs, device="cuda")
+        s.weigh(w.layer, q, sums, weights, window=w.window, sinks=w.sinks, offsets=d.offsets)
+        torch.cuda.synchronize()
+    check(out[:w.rows], want, bound)
+    check_lse(sums[:w.rows], lse, room)
+    assert bool((out[w.rows:] == 5).all()) and bool((sums[w.rows:] == 5).all())
+    got, off = w.weights(sums[:w.rows])
+    assert (np.abs(weights.double().cpu().numpy() - got) <= off).all()
+
+
 @pytest.mark.parametrize("kind", ["none", "out of range"])
 @pytest.mark.parametrize("seqs", [[(70, 30), (5, 0)], [(1, 99), (1, 4)]], ids=str)
 def test_blocks_behind_the_window_may_be_missing(torch, ck, seqs, kind):
