@@ -301,7 +301,8 @@ __device__ void move_entry(const EvictArgs& a, uint32_t i, const Entry& e) {
 // position j or later, so a token that is still to be read lies behind all that
 // have been written, and a batch is safe to write once all of it has been read.
 // Bound by memory: 8 sequences cut to 2048 tokens of 32 planes of 2 KiB, 2.1 GB read
-// and written but for what stays, in 461 us (95 % of a copy's rate).
+// and written but for what stays, in 450 us (98 % of a copy's rate; 461 us with loads
+// and stores that the caches keep, which hold a small part of it).
 template <typename V>
 __global__ void __launch_bounds__(kMove) k_evict_move(EvictArgs a) {
   constexpr uint32_t kBatch = kMove / 4 * kHeld;  // slices are 4 units wide at least
@@ -347,14 +348,17 @@ __global__ void __launch_bounds__(kMove) k_evict_move(EvictArgs a) {
 #pragma unroll
       for (uint32_t k = 0; k < kHeld; ++k) {
         dst[k] = in ? target[k * at_once + lane_token] : ~0ull;
-        if (dst[k] != ~0ull) held[k] = *(const V*)(base + source[k * at_once + lane_token] + (uint64_t)column * sizeof(V));
+        if (dst[k] != ~0ull)
+          held[k] = __builtin_nontemporal_load((const V*)(base + source[k * at_once + lane_token] +
+                                                          (uint64_t)column * sizeof(V)));
       }
 #pragma unroll
       for (uint32_t k = 0; k < kHeld; ++k) asm volatile("" : "+v"(held[k]));  // all of them have arrived
       __syncthreads();
 #pragma unroll
       for (uint32_t k = 0; k < kHeld; ++k)
-        if (dst[k] != ~0ull) *(V*)(base + dst[k] + (uint64_t)column * sizeof(V)) = held[k];
+        if (dst[k] != ~0ull)
+          __builtin_nontemporal_store(held[k], (V*)(base + dst[k] + (uint64_t)column * sizeof(V)));
     }
   }
 }

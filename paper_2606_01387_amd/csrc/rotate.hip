@@ -96,10 +96,10 @@ __device__ __forceinline__ float across_head(float x) {
 // and angles (one pair a lane, then LDS) are looked up.
 //
 // Bound by memory, and by those dependent reads where rows are few: 18348 rows of 28
-// query heads over 4 of 128, three axes, to e4m3 in 85 us, 3.8 TB/s read and written
-// (78 % of a copy's rate); four loads of a lane at a time, as 2 take 92 us, 3 83 or
-// 84, 9 95.  16384 rows of 32 heads over 8 of 64 in 48 us, 4.2 TB/s; 48 single rows
-// of 32 heads over 8 of 128 in 6.3 us.
+// query heads over 4 of 128, three axes, to e4m3 in 80 us, 4.0 TB/s read and written
+// (82 % of a copy's rate; 85 us with loads that the caches keep); four loads of a lane
+// at a time (2 took 92 us where 4 took 85, 9 95).  16384 rows of 32 heads over 8 of 64
+// in 43 us, 4.7 TB/s; 48 single rows of 32 heads over 8 of 128 in 6.3 us.
 template <int D, bool E4M3, bool NEIGHBOURS>
 __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
   constexpr uint32_t kLanes = D / 8, kHeads = 64 / kLanes, kMany = 4;
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
                              : h < a.q_heads + a.kv_heads
                                  ? a.k + row * a.k_row + (h - a.q_heads) * a.k_head
                                  : a.v + row * a.v_row + (h - a.q_heads - a.kv_heads) * a.v_head;
-      w[j] = *(const u32x4*)(from + at);
+      w[j] = __builtin_nontemporal_load((const u32x4*)(from + at));  // read once
     }
     if (h0 == part * kHeads) {
       qw = weights(a.q_norm, at);

@@ -237,8 +237,8 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 //
 // Bound by both units at once: 16 products and 96 vector operations of a wave take
 // 0.38 us together on a SIMD, 0.28 and 0.25 us alone.  8192 causal rows of 32 query
-// heads over 8 of 128 take 312 to 321 us (0.86 to 0.88 PFLOP/s of the pairs that are
-// seen), of which reading operands from LDS is some 50, copies to LDS 35, the masks on the
+// heads over 8 of 128 take 312 to 338 us on several cards (0.81 to 0.88 PFLOP/s of the
+// pairs that are seen), of which reading operands from LDS is some 50, copies to LDS 35, the masks on the
 // diagonal 15 and the beginnings of 2048 workgroups 20.  Eight waves to a workgroup:
 // 361 us; half or twice the chunks: 404 and 343 us; one phase after the other: 478 us.
 

@@ -13,8 +13,9 @@
 namespace {
 
 // Bound by the matrix cores and the vector unit beside them: 16384 rows of 32 query
-// heads over 8 of 128 in a window of 4096 behind 4 first tokens take 966 us, 1.0 PFLOP/s
-// of the pairs that are seen, the matrix cores 46 % busy.  Tiles with a mask cost a
+// heads over 8 of 128 in a window of 4096 behind 4 first tokens take 966 to 1028 us on
+// several cards, 0.94 to 1.0 PFLOP/s of the pairs that are seen, the matrix cores 46 %
+// busy.  Tiles with a mask cost a
 // short window the most: 12 ragged e4m3 prompts in a window of 1000 behind 20 took 257 us
 // when every wave looked through all of a masked tile's V for infinities and waited
 // for copies just begun, 183 us with its own part and the copies of a tile before.
