@@ -735,7 +735,8 @@ int claim_attend_window(claim_pool* pool, const claim_seqs* seqs, const claim_wi
  * it: that is the program's to do before the row is used again.
  *
  * weights_stride is at least max_blocks * block_size; limits as for claim_attend, and
- * max_blocks * block_size below 2^31.  work: claim_weigh_work bytes, 256-byte aligned
+ * max_blocks * block_size below 2^31, num_seqs x num_kv_heads x that / 256 below 2^24
+ * where sequences have many rows.  work: claim_weigh_work bytes, 256-byte aligned
  * (it goes by max_blocks and the counts alone; it may be 0, work NULL). */
 typedef struct claim_weigh_desc {
   claim_kv_desc kv; /* v_scale is not used */

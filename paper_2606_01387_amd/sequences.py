@@ -135,7 +135,8 @@ class Sequences:
         ``tokens`` tokens keep the first ``sinks``, the last ``recent`` and of the
         others those of the largest ``weights`` (float32, as for :meth:`weigh`;
         they come along).  Returns the device tensors of statuses and of the
-        kept tokens' old positions [n, tokens] (NONE past the new lengths)."""
+        kept tokens' old positions [n, tokens] (NONE past the new lengths).
+        Scratch is taken and kept as :meth:`attend` does."""
         at = 0 if ids is None else self._ints("ids", ids)
         n = self.tables.shape[0] if ids is None else ids.numel()
         if not 1 <= tokens < 1 << 31 or sinks < 0 or recent < 0 or sinks + recent > tokens:
@@ -234,7 +235,8 @@ class Sequences:
         ``window`` positions (its own among them; None: all) and the first
         ``sinks``.  Table entries of other positions are not read.  With
         ``lse`` (float32 [rows, heads]), the logarithms of the rows' sums of
-        exponentials are written there, for :meth:`weigh`."""
+        exponentials are written there, for :meth:`weigh`.  Scratch is taken
+        and kept as :meth:`attend` does."""
         return self._attend(layer, q, None, 0, 0, ids, offsets, scale, k_scale, v_scale, out,
                             (*self._window(window, sinks), lse))
 
@@ -256,7 +258,8 @@ class Sequences:
         for the rows of ``q``, whose logarithms ``lse`` :meth:`attend_window` gave
         with the same window, sinks and scales.  ``q`` and ``lse`` may be a
         prompt's last rows alone.  :meth:`fork` does not copy a row of weights,
-        and :meth:`free` does not clear it."""
+        and :meth:`free` does not clear it.  Scratch is taken and kept as
+        :meth:`attend` does."""
         shape = q.shape
         if len(shape) != 3:
             raise ValueError("q must be [rows, heads, head_dim]")
@@ -294,6 +297,8 @@ class Sequences:
         pool = self.pool
         record.pack_into(self._desc, 0, *given, self._work_at, self._work_bytes, *more)
         rc = call(pool._h, self._seqs_ref, self._desc_at)
+        if rc == OK:
+            return
         if rc == ENOSPC:  # the first call of a larger shape
             need = ctypes.c_uint64()
             _check(work(pool._h, self._seqs_ref, self._desc_at, ctypes.byref(need)), work.__name__)
