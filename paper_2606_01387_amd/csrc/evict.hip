@@ -214,7 +214,8 @@ __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
     __syncthreads();
     const uint32_t stay = gone < a.tokens ? gone : a.tokens;
     // a last block that is not full will be written: it must be the sequence's own
-    const uint32_t first = stay < a.tokens || a.tokens % a.bs ? (stay < a.tokens ? stay : a.tokens - 1) / a.bs : a.blocks;
+    const bool writes = stay < a.tokens || a.tokens % a.bs;
+    const uint32_t first = writes ? (stay < a.tokens ? stay : a.tokens - 1) / a.bs : a.blocks;
     if (wave == 0) {
       uint32_t need = 0;
       for (uint32_t j = first; j < a.blocks; j += 64) {
@@ -429,7 +430,8 @@ int claim_seqs_evict(claim_pool* P, const claim_seqs* s, const claim_evict_desc*
   // slices as wide as a token, narrower where that leaves CUs idle
   a.width = 4;
   while (a.width < 64 && a.width < a.token_units) a.width *= 2;
-  while (a.width > 16 && (uint64_t)d->n * a.planes * ((a.token_units + a.width - 1) / a.width) < 4ull * p.cus) a.width /= 2;
+  while (a.width > 16 && (uint64_t)d->n * a.planes * ((a.token_units + a.width - 1) / a.width) < 4ull * p.cus)
+    a.width /= 2;
   a.slices = (a.token_units + a.width - 1) / a.width;
   SEQ_HIP(hipSetDevice(p.device));
   if (d->ids && d->n > kLookThrough) {

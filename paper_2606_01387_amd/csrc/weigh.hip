@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
               else
                 w = key[n][t];
               score[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w),
-                                                                 __builtin_bit_cast(bf16x8, query[t]), score[n], 0, 0, 0);
+                                                                 __builtin_bit_cast(bf16x8, query[t]),
+                                                                 score[n], 0, 0, 0);
             }
           }
           const bool counts = col.lse < __builtin_inff();
@@ -325,7 +326,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       for (uint32_t i = 0; i < kLooks; ++i)
         copy_to_lds(from, ends && !has[i] ? chunk_at : look[i],
                     lds_address(ring) + slot * F::kTile + (i * kManyWaves + wave) * 1024);
-      copy_words_to_lds(sums_from, ends && !has_log ? 0 : log, lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
+      copy_words_to_lds(sums_from, ends && !has_log ? 0 : log,
+                        lds_address((const uint8_t*)sums) + slot * kManyColumns * 4);
     };
     fetch(n, 0);
     fetch(n + 1, 1);
@@ -370,7 +372,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
       for (int i = 0; i < kSteps; ++i) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w[i]), score[u], 0, 0, 0);
+          score[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[u][i], __builtin_bit_cast(bf16x8, w[i]),
+                                                             score[u], 0, 0, 0);
         if (i + 2 < kSteps) read(at, i + 2); else read(after, i + 2 - kSteps);
 #pragma unroll
         for (int e = 32 / kSteps * i; e < 32 / kSteps * (i + 1); ++e) {
@@ -403,7 +406,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
     // every key in full_from .. full_to - 1
     const auto down = [&](int64_t x) { return x > 0 ? (x < 0xFFFFFFFF ? (uint32_t)x : 0xFFFFFFFFu) / rows : 0; };
     const auto up = [&](int64_t x) { return down(x + rows - 1); };
-    uint32_t seen_from = down(pos - before), full_from = up(pos + 63ll - before), seen_to = ~0u, full_to = it.n / rows;
+    uint32_t seen_from = down(pos - before), seen_to = ~0u;
+    uint32_t full_from = up(pos + 63ll - before), full_to = it.n / rows;
     if (pos >= a.sinks) seen_to = up(pos + 63ll - before + a.window);
     if (pos + 63 >= a.sinks) {
       const uint32_t x = down((int64_t)pos - before + a.window);
@@ -415,8 +419,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) k_weigh_rows(WeighArgs a) 
     full_to = uniform(full_to);
     const auto seen = [&](uint32_t m) { return m >= seen_from && m < seen_to; };
     // Half by half: (n - 1, 1) is weighed with the products of (n, 0), (n, 0) with those
-    // of (n, 1).  Tile n is there before it is needed: all waves meet, a tile ahead,
-    // when its copies have arrived and tile n - 2 has been read.
+    // of (n, 1).  All waves meet before (n, 0) when the copies of tile n + 1 have arrived
+    // and tile n - 1 has been read, whose place tile n + 3 takes.
     uint32_t slot = 0;  // tile n's
     f32x16 one[2] = {}, two[2] = {};
     float l1 = __builtin_inff();  // of the half before the first: it adds nothing
@@ -539,8 +543,8 @@ int launch(const PoolView& p, const WeighPlan& plan, const WeighArgs& a) {
   if (!plan.many) {
     hipLaunchKernelGGL((k_weigh_few<D, E4M3>), dim3(a.num_seqs * a.tiles), dim3(256), 0, p.stream, a);
   } else {
-    hipLaunchKernelGGL((k_weigh_rows<D, E4M3>), dim3(a.num_seqs * a.tiles * a.chunks * a.heads), dim3(64 * kManyWaves), 0,
-                       p.stream, a);
+    hipLaunchKernelGGL((k_weigh_rows<D, E4M3>), dim3(a.num_seqs * a.tiles * a.chunks * a.heads),
+                       dim3(64 * kManyWaves), 0, p.stream, a);
     const uint32_t most = 32 * p.cus / a.num_seqs + 1, need = (a.room + 63) / 64;
     const uint32_t groups = need < most ? need : most;
     hipLaunchKernelGGL(k_weigh_join, dim3(a.num_seqs * groups), dim3(64), 0, p.stream, a, groups);

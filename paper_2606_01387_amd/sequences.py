@@ -14,7 +14,8 @@ import ctypes
 import struct
 
 from . import claimkv
-from .claimkv import CAttendDesc, CEvictDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWeighDesc, CWindowDesc, ENOSPC, OK, _check, _torch, lib
+from .claimkv import (CAttendDesc, CEvictDesc, CKvDesc, CRotateDesc, CRows, CSeqs, CWeighDesc, CWindowDesc,
+                      ENOSPC, OK, _check, _torch, lib)
 
 SEQ_OK, SEQ_NO_BLOCKS, SEQ_REFUSED = 0, 1, 2
 NONE = -1  # a table entry that names no block (0xFFFFFFFF in 32 bits)
