@@ -81,6 +81,22 @@ __device__ __forceinline__ float sum_head(float x) {
   return LANES == 16 ? x + lane_rule<0x140>(x) : x;  // 15 - lane of sixteen
 }
 
+// The mean square of a head, of which a lane has eight elements.
+template <int D>
+__device__ __forceinline__ float mean_square(const Eight& y) {
+  float square = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) square = __builtin_fmaf(y.x[i], y.x[i], square);
+  return sum_head<D / 8>(square) * (1.0f / D);
+}
+
+// A mean square with eps below 2^-90 may be the sum of squares that have lost bits at
+// the lower end of 32, or all of them: such a head is taken 2^100 times as large, which
+// rounds nothing and cancels in x / sqrt(mean(x^2) + eps).  With an eps of 2^-90 or more
+// no mean is that small, and the kernel does not look (SMALL): 79.2 us in place of 81.1
+// for the e4m3 prompts below.
+constexpr float kSmall = 0x1p-90f, kUp = 0x1p100f;
+
 // The value of the head's lane half of its lanes on.
 template <uint32_t LANES>
 __device__ __forceinline__ float across_head(float x) {
@@ -100,7 +116,7 @@ __device__ __forceinline__ float across_head(float x) {
 // (82 % of a copy's rate; 85 us with loads that the caches keep); four loads of a lane
 // at a time (2 took 92 us where 4 took 85, 9 95).  16384 rows of 32 heads over 8 of 64
 // in 43 us, 4.7 TB/s; 48 single rows of 32 heads over 8 of 128 in 6.3 us.
-template <int D, bool E4M3, bool NEIGHBOURS>
+template <int D, bool E4M3, bool NEIGHBOURS, bool SMALL>
 __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
   constexpr uint32_t kLanes = D / 8, kHeads = 64 / kLanes, kMany = 4;
   __shared__ float2 angles[4][D / 2];
@@ -170,15 +186,21 @@ __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
       const Eight y = widen(mine);
       Eight o = y;
       if (__any(!is_v)) {
-        float square = 0;
+        const bool normed = !is_v && (is_q ? a.q_norm : a.k_norm);
+        Eight z = y;
+        float mean = mean_square<D>(y) + a.eps;
+        const bool small = normed && mean < kSmall;
+        if (SMALL && __any(small)) {
+          const float up = small ? kUp : 1.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) square = __builtin_fmaf(y.x[i], y.x[i], square);
-        square = sum_head<kLanes>(square);
-        const float f = (is_q ? a.q_norm : a.k_norm) ? rsqrtf(square * (1.0f / D) + a.eps) : 1.0f;
+          for (int i = 0; i < 8; ++i) z.x[i] *= up;
+          mean = mean_square<D>(z) + a.eps * up * up;
+        }
+        const float f = normed ? rsqrtf(mean) : 1.0f;
         const Eight own = widen(is_q ? qw : kw);
         Eight p, r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p.x[i] = y.x[i] * f * own.x[i];
+        for (int i = 0; i < 8; ++i) p.x[i] = z.x[i] * f * own.x[i];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           r.x[i] = NEIGHBOURS ? p.x[i ^ 1] : whole ? across_head<kLanes>(p.x[i]) : __shfl(p.x[i], other_lane);
@@ -207,13 +229,21 @@ __global__ void __launch_bounds__(256) k_write_rotated(Rotate a, Places s) {
   }
 }
 
+template <int D, bool E4M3, bool NEIGHBOURS>
+void launch(const PoolView& p, const Rotate& a, const Places& s) {
+  const dim3 grid((uint32_t)(((uint64_t)a.rows * a.waves + 3) / 4));
+  if (a.eps < kSmall && (a.q_norm || a.k_norm))
+    hipLaunchKernelGGL((k_write_rotated<D, E4M3, NEIGHBOURS, true>), grid, dim3(256), 0, p.stream, a, s);
+  else
+    hipLaunchKernelGGL((k_write_rotated<D, E4M3, NEIGHBOURS, false>), grid, dim3(256), 0, p.stream, a, s);
+}
+
 template <int D, bool E4M3>
 void launch(const PoolView& p, const Rotate& a, const Places& s, bool neighbours) {
-  const dim3 grid((uint32_t)(((uint64_t)a.rows * a.waves + 3) / 4));
   if (neighbours)
-    hipLaunchKernelGGL((k_write_rotated<D, E4M3, true>), grid, dim3(256), 0, p.stream, a, s);
+    launch<D, E4M3, true>(p, a, s);
   else
-    hipLaunchKernelGGL((k_write_rotated<D, E4M3, false>), grid, dim3(256), 0, p.stream, a, s);
+    launch<D, E4M3, false>(p, a, s);
 }
 
 int check_rotate(const PoolView& p, const claim_seqs* s, const claim_rotate_desc* d) {
