@@ -710,7 +710,12 @@ int claim_attend(claim_pool* pool, const claim_seqs* seqs, const claim_attend_de
  * With lse (float [num_rows][num_heads], may be NULL) each row's and head's
  * logarithm of sum_p exp(scale * k_scale * q . k_p) is written there, for
  * claim_weigh: -infinity where nothing is seen, NaN where the output is NaN for a
- * missing block or a score that is NaN or +infinity. */
+ * missing block or a score that is NaN or +infinity.
+ *
+ * No block is given up here: a program that lets blocks behind the window go edits its
+ * tables and counts itself, and such a sequence is no longer one that claim_seqs_evict
+ * cuts (a position without a block).  work goes by max_blocks, the counts, window and
+ * sinks. */
 typedef struct claim_window_desc {
   claim_attend_desc attend; /* work: claim_attend_window_work bytes */
   uint32_t window;
@@ -737,7 +742,8 @@ int claim_attend_window(claim_pool* pool, const claim_seqs* seqs, const claim_wi
  * weights_stride is at least max_blocks * block_size; limits as for claim_attend, and
  * max_blocks * block_size below 2^31, num_seqs x num_kv_heads x that / 256 below 2^24
  * where sequences have many rows.  work: claim_weigh_work bytes, 256-byte aligned
- * (it goes by max_blocks and the counts alone; it may be 0, work NULL). */
+ * (it goes by max_blocks, the counts and whether a stride of q is 2^24 or more; it may
+ * be 0, work NULL). */
 typedef struct claim_weigh_desc {
   claim_kv_desc kv; /* v_scale is not used */
   claim_rows q;

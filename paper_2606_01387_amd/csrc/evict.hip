@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(256) k_owner_first(uint32_t* owner, const uint
 // place, and of those equal to it the first ones.  Waves take runs of positions,
 // count, and then write what they keep in order.  Bound by dependent reads (length,
 // table and weights, counts) and the digits' barriers: 11 us for 200 tokens, 16 us
-// for 4000.
+// for 4000, 32 for 16000; 61 us for 16000 of one weight, which are counted in one place.
 __global__ void __launch_bounds__(kPlan) k_evict_select(EvictArgs a) {
   __shared__ uint32_t above[kPlan / 64], same[kPlan / 64], gone;
   const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;

@@ -134,7 +134,8 @@ __device__ __forceinline__ float sum16(float x) {
 // to 8192 tokens, 8 KV heads of 128 for 4 query heads each, in 126 us, 4.9 TB/s.  Half
 // of the keys on their way while the other half is weighed takes more registers and
 // 134 us; what is left is the order of the loads, 64 bytes of 16 keys each: whole keys
-// one after another would take 118 us, but not lie as the products need them.
+// one after another would take 118 us, but not lie as the products need them.  The same
+// in e4m3 takes 85 us, 3.6 TB/s.
 
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
@@ -242,6 +243,9 @@ __global__ void __launch_bounds__(256) k_weigh_few(WeighArgs a) {
 // pairs that are seen), of which reading operands from LDS is some 50, copies to LDS 35, the masks on the
 // diagonal 15 and the beginnings of 2048 workgroups 20.  Eight waves to a workgroup:
 // 361 us; half or twice the chunks: 404 and 343 us; one phase after the other: 478 us.
+// The same in e4m3 takes 317 to 326 us.  In a window two compares a pair and nine words
+// of a lane that do not stay in registers (of 256, heads of 128) set the pace: the same
+// rows in a window of 4096 take 287 to 293 us and in one of 512 191 to 194.
 
 constexpr uint32_t kManyWaves = 4, kManyKeys = 64 * kManyWaves, kManyColumns = 64;
 
@@ -496,6 +500,16 @@ struct WeighPlan {
   uint32_t tiles, chunks;
 };
 
+// One kernel for a call, by the mean of its sequences' columns, as the host knows no
+// more of them: k_weigh_few where a tile of 64 columns holds a sequence's.  Where
+// sequences differ much, some of them get the wrong one.  8 KV heads of 128 for 4 query
+// heads each, all behind 4000 tokens: 63 single tokens take 103 to 107 us, a chunk of 512
+// rows 50 and of 4096 rows 241 to 250; the tokens with the chunk of 512, by k_weigh_few,
+// 500 us, with the one of 4096, by k_weigh_rows, 677.
+//
+// Tiles and chunks go by what a table can hold, so that work of one size does for any
+// lengths: the prompt of 8192 above takes 654 us in a table of 131072 positions, where
+// its empty tiles leave it one chunk, and the 64 single tokens 145 us in such tables.
 WeighPlan make_weigh_plan(const PoolView& p, const claim_seqs* s, const claim_weigh_desc* d) {
   WeighPlan r{};
   const uint64_t group = d->num_heads / p.heads, rows = d->kv.num_rows, seqs = d->kv.num_seqs;

@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(512, 2) k_window_rows(WindowArgs a) {
 
 // Bound by memory: 64 single tokens of 32 query heads over 8 of 128 in a window of 4096
 // read 1.0 GB of keys and values in 183 us, 5.5 TB/s; twice as many workgroups, with
-// their parts joined, take as long.
+// their parts joined, take as long.  The same in e4m3 takes 112 us, 4.5 TB/s.
 template <int D, bool E4M3, Within WITHIN, int QT>
 __global__ void __launch_bounds__(256, 2) k_window_few(WindowArgs a) {
   __shared__ typename Few<D, E4M3, 4>::WithSums shared;
@@ -42,6 +42,11 @@ struct WindowPlan {
   uint64_t parts;  // parts of all rows and heads; 0: none are kept
 };
 
+// One kernel for a call, by the mean of its sequences' query rows, as the host knows no
+// more of them: few_rows up to 64.  Where sequences differ much, some of them get the
+// wrong one.  32 heads over 8 of 128 in a window of 4096 behind 4000 tokens: 63 single
+// tokens take 221 us, a chunk of 512 rows 67 and of 4096 rows 288 to 300; the tokens with
+// the chunk of 512, by few_rows, 319 us, with the one of 4096, by many_rows, 528 to 553.
 WindowPlan make_window_plan(const PoolView& p, const claim_seqs* s, const claim_window_desc* w) {
   const claim_attend_desc* d = &w->attend;
   WindowPlan r{};

@@ -136,7 +136,8 @@ class Sequences:
         ``tokens`` tokens keep the first ``sinks``, the last ``recent`` and of the
         others those of the largest ``weights`` (float32, as for :meth:`weigh`;
         they come along).  Returns the device tensors of statuses and of the
-        kept tokens' old positions [n, tokens] (NONE past the new lengths).
+        kept tokens' old positions [n, tokens] (NONE past the new lengths), which
+        is as long as ``tokens`` says, whatever the tables hold.
         Scratch is taken and kept as :meth:`attend` does."""
         at = 0 if ids is None else self._ints("ids", ids)
         n = self.tables.shape[0] if ids is None else ids.numel()
@@ -234,7 +235,8 @@ class Sequences:
                       v_scale: float = 1.0, out=None):
         """claim_attend_window: :meth:`attend` where a row sees the last
         ``window`` positions (its own among them; None: all) and the first
-        ``sinks``.  Table entries of other positions are not read.  With
+        ``sinks``.  Table entries of other positions are not read, but their
+        blocks are not given up (:meth:`evict` does that).  With
         ``lse`` (float32 [rows, heads]), the logarithms of the rows' sums of
         exponentials are written there, for :meth:`weigh`.  Scratch is taken
         and kept as :meth:`attend` does."""
